@@ -329,6 +329,69 @@ pac_status pac_quantize_absmax(int device, void* cuda_stream, const float* dev_x
 pac_status pac_dequantize_absmax(int device, void* cuda_stream, const signed char* dev_q, const float* dev_c, long long n,
                                  int block, float* dev_out);
 
+/* Microscaled 4-bit floating point (MXFP4, OCP microscaling formats) for frozen matrices and hidden states, beside the
+ * INT8 codec above (Section IV-D keeps the frozen backbone in few bits).  Rows are cut into blocks of 32 columns; a block has
+ * one power of two, 2^(s - 127), and every value is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7; 8..15 negative):
+ *     s = max(floor(log2(absmax)) - 2, -127) + 127,   value = nearest (ties to the even code; beyond 6: 6) of x 2^(127 - s)
+ * A block of zeros has s = 0; a block with an infinity or a NaN gets s = 255 and codes 0 and reads back as 32 NaN.
+ *
+ * dev_codes: [rows][16 * ceil(cols / 32)] bytes, the even column in the low half of a byte, zeros past the last column.
+ * dev_scales: [ceil(rows / 128)][2 * ceil(cols / 256)][32][4][4] bytes; byte [R][C][i][j][b] is s of row 128 R + 32 j + i and
+ * columns 32 (4 C + b) and following; entries past the last row or column are written as 0, and a caller who makes scales in
+ * another way puts anything but 255 there.  Both 16-byte aligned.  dtype (PAC_F32, PAC_BF16) is that of the values, whose rows
+ * are ldx (ldo) >= cols elements apart and aligned to an element; 32-byte aligned rows are the fast case.
+ *
+ * These calls and those below enqueue on cuda_stream (NULL: the default stream) of `device`, leave the caller's current device
+ * as it was, allocate nothing, keep nothing and may be captured into a graph.  No rows: nothing is done.  Errors:
+ * PAC_ERR_INVALID_ARG for NULL or misaligned pointers, unknown types, cols < 1 or a pitch below it; PAC_ERR_CUDA. */
+pac_status pac_quantize_mxfp(int device, void* cuda_stream, const void* dev_x, int dtype, long long rows, int cols, long long ldx,
+                             unsigned char* dev_codes, unsigned char* dev_scales);
+pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const unsigned char* dev_codes, const unsigned char* dev_scales,
+                               long long rows, int cols, void* dev_out, int dtype, long long ldo);
+
+/* y = x W^T for a frozen matrix W [N][K] in MXFP4: dev_x [M][K], dev_y [M][N], either in fp32 or bf16 with any pitch and
+ * alignment of an element.  The values of W and of x enter exactly, sums are fp32, y is rounded once.  bf16 rows of x on
+ * 16-byte boundaries are the fast case.  Every sum has a fixed order.  Conventions as above.  (Waits inside the kernel are
+ * bounded; one that ran out, after about a second, leaves NaN in its part of y.) */
+pac_status pac_mxfp_linear(int device, void* cuda_stream, const void* dev_x, int x_dtype, int M, long long ldx,
+                           const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_y, int y_dtype,
+                           long long ldy);
+/* Its backward pass: dx = dy W, dev_dy [M][N], dev_dx [M][K].  W is frozen and has no gradient. */
+pac_status pac_mxfp_linear_grad(int device, void* cuda_stream, const void* dev_dy, int dy_dtype, int M, long long lddy,
+                                const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_dx,
+                                int dx_dtype, long long lddx);
+
+/* y = A B^T [M][N] of two matrices in MXFP4, A [M][K] and B [N][K]: block-scaled tensor-core products of the codes as they are,
+ * sums in fp32, y rounded once (hidden states quantised on the way into a frozen matrix).  Scales as pac_quantize_mxfp leaves
+ * them: the codes past the last column are 0 and their scales anything but 255.  Conventions as above. */
+pac_status pac_mxfp_product(int device, void* cuda_stream, const unsigned char* dev_a_codes, const unsigned char* dev_a_scales, int M,
+                            const unsigned char* dev_b_codes, const unsigned char* dev_b_scales, int N, int K, void* dev_y, int y_dtype,
+                            long long ldy);
+
+/* One AdamW step (as pac_adam_step) over a list of tensors, fp32 or bf16 parameters and gradients, in one launch per 480 tensors:
+ *     m = b1 m + (1-b1) g;  v = b2 v + ((1-b2) g) g;  p = (p - lr wd p) - lr (m / bc1) / (sqrt(v / bc2) + eps)
+ * with g times grad_scale, wd where decay is not 0, bf16 parameters rounded to the nearest.  state_bits 32: m and v are fp32 [n]
+ * and every rounding is that of pac_adam_step.  state_bits 8: m and sqrt(v) are float8 codes (E4M3, one byte) [n] times
+ * m_scale, v_scale: fp32 [ceil(n / 256)], one constant (absmax / 448) per 256 elements.  Codes are rounded up or down by random
+ * bits, a function of (seed, step, place in the list, element): equal calls give equal codes, averages stay unbiased.  A root
+ * above 0 is never rounded to 0.  Blocks below 2^-100 become 0; a block whose new moment is not finite gets the constant NaN.
+ *
+ * tensors: HOST array of `count` entries, read during the call; its pointers are device memory that no other entry may overlap.
+ * Pointers aligned to eight elements are the fast case, one element is enough.  step: the number of this step, from 1.
+ * dev_step: device, its number there instead (read by the kernel; the caller moves it on), which a captured step needs: a
+ * call under capture without it is refused with PAC_ERR_BAD_STATE.  hp, grad_scale and the list are as they were at capture.
+ * Errors: PAC_ERR_INVALID_ARG for NULL or misaligned pointers, negative sizes, unknown types or bits, step < 1. */
+typedef struct {
+    void* p; const void* g;
+    void* m; void* v;
+    float* m_scale; float* v_scale;   /* state_bits 8 */
+    long long n;
+    int p_dtype, g_dtype;             /* PAC_F32 or PAC_BF16 */
+    int decay;
+} pac_adamw_tensor;
+pac_status pac_adamw_tensors(int device, void* cuda_stream, const pac_adamw_tensor* tensors, int count, int state_bits,
+                             const pac_adamw* hp, long long step, const long long* dev_step, float grad_scale, unsigned seed);
+
 /* Evaluation forward that allocates nothing (the paper has no counterpart; this is a
  * packaging variant of pac_eval_logits for the mean-pool classifier head).
  *

@@ -28,7 +28,8 @@ EXPORTS = ["pac_create", "pac_destroy", "pac_cache_register", "pac_cache_registe
            "pac_adam_step", "pac_eval_logits", "pac_gather", "pac_train_epoch", "pac_train_epoch_dev",
            "pac_param_count", "pac_get_params", "pac_set_params", "pac_get_grads", "pac_get_opt_state",
            "pac_set_opt_state", "pac_set_option", "pac_device_buffers", "pac_params_changed", "pac_kernel_times", "pac_stream_phase_times", "pac_launch_count", "pac_sync", "pac_selftest_wait_expiry", "pac_selftest_rows_plan", "pac_selftest_second_pass_plan", "pac_last_error",
-           "pac_kernel_path", "pac_eval_logits_static", "pac_quantize_absmax", "pac_dequantize_absmax"]
+           "pac_kernel_path", "pac_eval_logits_static", "pac_quantize_absmax", "pac_dequantize_absmax",
+           "pac_quantize_mxfp", "pac_dequantize_mxfp", "pac_mxfp_linear", "pac_mxfp_linear_grad", "pac_mxfp_product", "pac_adamw_tensors"]
 
 
 class PacError(RuntimeError):
@@ -47,6 +48,11 @@ class _AdapterCfg(C.Structure):
 class _AdamW(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("weight_decay", C.c_float)]
+
+
+class _AdamWTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n", C.c_longlong), ("p_dtype", C.c_int), ("g_dtype", C.c_int), ("decay", C.c_int)]
 
 
 @dataclasses.dataclass
@@ -114,6 +120,14 @@ def load_library() -> C.CDLL:
     lib.pac_quantize_absmax.restype = I
     lib.pac_dequantize_absmax.argtypes = [I, P, P, P, LL, I, P]
     lib.pac_dequantize_absmax.restype = I
+    lib.pac_quantize_mxfp.argtypes = [I, P, P, I, LL, I, LL, P, P]
+    lib.pac_dequantize_mxfp.argtypes = [I, P, P, P, LL, I, P, I, LL]
+    lib.pac_mxfp_linear.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL]
+    lib.pac_mxfp_linear_grad.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL]
+    lib.pac_mxfp_product.argtypes = [I, P, P, P, I, P, P, I, I, P, I, LL]
+    lib.pac_adamw_tensors.argtypes = [I, P, C.POINTER(_AdamWTensor), I, I, C.POINTER(_AdamW), LL, P, F, C.c_uint]
+    for name in ("pac_quantize_mxfp", "pac_dequantize_mxfp", "pac_mxfp_linear", "pac_mxfp_linear_grad", "pac_mxfp_product", "pac_adamw_tensors"):
+        getattr(lib, name).restype = I
     lib.pac_last_error.argtypes = [P]
     lib.pac_last_error.restype = C.c_char_p
     lib.pac_kernel_path.argtypes = [P]
@@ -469,3 +483,212 @@ def dequantize_absmax(q, c, block: int, device: int = 0, stream: Optional[int] =
     if st != 0:
         raise PacError(st, "pac_dequantize_absmax failed")
     return out
+
+
+# ---------------------------------------------------------------------------
+# MXFP4: frozen matrices and hidden states in 4 bits, and products with them.  Every call runs on the device of its
+# tensors and on torch's current stream there.
+# ---------------------------------------------------------------------------
+def _invalid(what: str, ok: bool):
+    if not ok:
+        raise PacError(1, what)
+
+
+def _dtype(t):
+    import torch
+    code = {torch.float32: PAC_F32, torch.bfloat16: PAC_BF16}.get(t)
+    _invalid(f"values are float32 or bfloat16, not {t}", code is not None)
+    return code
+
+
+def _stream(device):
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _rows(t, name: str):
+    """A CUDA matrix with consecutive elements along its rows: (rows, columns, elements from row to row)."""
+    _invalid(f"{name} is a 2-D CUDA tensor", t.is_cuda and t.dim() == 2)
+    rows, cols = t.shape
+    _invalid(f"{name} has at least one column", cols > 0)
+    if rows <= 1:
+        _invalid(f"{name}: elements of a row are consecutive", cols == 1 or t.stride(1) == 1 or t.numel() == 0)
+        return rows, cols, cols
+    _invalid(f"{name}: elements of a row are consecutive, rows do not overlap", (cols == 1 or t.stride(1) == 1) and t.stride(0) >= cols)
+    return rows, cols, t.stride(0)
+
+
+def mxfp_shapes(rows: int, cols: int):
+    """Shapes of the codes and of the scales (both uint8) of a rows x cols matrix."""
+    return (rows, 16 * ((cols + 31) // 32)), ((rows + 127) // 128, 2 * ((cols + 255) // 256), 32, 4, 4)
+
+
+def _mxfp(codes, scales, cols: int, device=None):
+    """Rows of an MXFP4 matrix of `cols` columns, its layout checked."""
+    import torch
+    _invalid("codes and scales are contiguous CUDA uint8 tensors", codes.is_cuda and scales.is_cuda and codes.dtype == scales.dtype == torch.uint8
+             and codes.dim() == 2 and codes.is_contiguous() and scales.is_contiguous() and cols > 0)
+    rows = codes.shape[0]
+    want = mxfp_shapes(rows, cols)
+    _invalid(f"{rows} x {cols} values have codes and scales of shapes {want}, not {tuple(codes.shape)} and {tuple(scales.shape)}",
+             tuple(codes.shape) == want[0] and tuple(scales.shape) == want[1])
+    _invalid("all tensors are on one device", codes.device == scales.device and (device is None or codes.device == device))
+    return rows
+
+
+def _out(out, rows: int, cols: int, dtype, device):
+    """The tensor that receives a result, made here when the caller gives none."""
+    import torch
+    if out is None:
+        return torch.empty((rows, cols), dtype=dtype, device=device), cols
+    _invalid(f"out is {rows} x {cols} {dtype} on {device}", tuple(out.shape) == (rows, cols) and out.dtype == dtype and out.device == device)
+    return out, _rows(out, "out")[2]
+
+
+def quantize_mxfp(x, codes=None, scales=None):
+    """(codes, scales) of a CUDA matrix, float32 or bfloat16, whose rows may lie apart: microscaled 4-bit floating point, one power
+    of two per 32 columns.  Shapes as mxfp_shapes gives; codes and scales may be given to be written into."""
+    import torch
+    rows, cols, ld = _rows(x, "x")
+    shapes = mxfp_shapes(rows, cols)
+    if codes is None:
+        codes = torch.empty(shapes[0], dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty(shapes[1], dtype=torch.uint8, device=x.device)
+    _invalid(f"codes have {shapes[0][0]} rows", _mxfp(codes, scales, cols, x.device) == rows)
+    st = load_library().pac_quantize_mxfp(x.device.index, _stream(x.device), x.data_ptr(), _dtype(x.dtype), rows, cols, ld, codes.data_ptr(), scales.data_ptr())
+    if st != 0:
+        raise PacError(st, "pac_quantize_mxfp failed")
+    return codes, scales
+
+
+def dequantize_mxfp(codes, scales, cols: int, dtype=None, out=None):
+    """The matrix [rows][cols] that codes and scales stand for, bfloat16 (exact) or float32."""
+    import torch
+    rows = _mxfp(codes, scales, cols)
+    dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
+    code = _dtype(dtype)
+    out, ld = _out(out, rows, cols, dtype, codes.device)
+    st = load_library().pac_dequantize_mxfp(codes.device.index, _stream(codes.device), codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), code, ld)
+    if st != 0:
+        raise PacError(st, "pac_dequantize_mxfp failed")
+    return out
+
+
+def _mxfp_linear(name: str, x, codes, scales, N: int, K: int, cols: int, dtype, out):
+    M, _, ld = _rows(x, "x")
+    dtype = dtype or (out.dtype if out is not None else x.dtype)
+    xt, yt = _dtype(x.dtype), _dtype(dtype)
+    out, ldo = _out(out, M, cols, dtype, x.device)
+    st = getattr(load_library(), name)(x.device.index, _stream(x.device), x.data_ptr(), xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K,
+                                       out.data_ptr(), yt, ldo)
+    if st != 0:
+        raise PacError(st, f"{name} failed")
+    return out
+
+
+def mxfp_linear(x, codes, scales, dtype=None, out=None):
+    """y = x W^T [M][N] for x [M][K] and a frozen W [N][K] in MXFP4 (quantize_mxfp); x and y float32 or bfloat16."""
+    K = _rows(x, "x")[1]
+    N = _mxfp(codes, scales, K, x.device)
+    _invalid("W has at least one row", N > 0)
+    return _mxfp_linear("pac_mxfp_linear", x, codes, scales, N, K, N, dtype, out)
+
+
+def mxfp_linear_grad(dy, codes, scales, cols: int, dtype=None, out=None):
+    """The backward pass of mxfp_linear: dx = dy W [M][cols] for dy [M][N]; W is frozen and has no gradient."""
+    N = _mxfp(codes, scales, cols, dy.device)
+    _invalid(f"dy has {N} columns, one per row of W", _rows(dy, "dy")[1] == N)
+    return _mxfp_linear("pac_mxfp_linear_grad", dy, codes, scales, N, cols, cols, dtype, out)
+
+
+def mxfp_product(a_codes, a_scales, b_codes, b_scales, cols: int, dtype=None, out=None):
+    """A B^T [M][N] of two MXFP4 matrices of `cols` columns each, bfloat16 or float32."""
+    import torch
+    M, N = _mxfp(a_codes, a_scales, cols), _mxfp(b_codes, b_scales, cols, a_codes.device)
+    _invalid("B has at least one row", N > 0)
+    dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
+    code = _dtype(dtype)
+    out, ldo = _out(out, M, N, dtype, a_codes.device)
+    st = load_library().pac_mxfp_product(a_codes.device.index, _stream(a_codes.device), a_codes.data_ptr(), a_scales.data_ptr(), M, b_codes.data_ptr(),
+                                         b_scales.data_ptr(), N, cols, out.data_ptr(), code, ldo)
+    if st != 0:
+        raise PacError(st, "pac_mxfp_product failed")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# AdamW over a list of tensors
+# ---------------------------------------------------------------------------
+class AdamWTensors:
+    """AdamW over a list of CUDA tensors (float32 or bfloat16, contiguous, all on one device) with moments in float32 (bits=32) or
+    in 8 bits (bits=8: float8_e4m3fn codes, the second moment as its root, one float32 constant per 256 elements).
+
+    params and grads are borrowed; step() reads the grads and updates the params and the moments in place, in one launch on torch's
+    current stream.  state: dict of lists "m", "v" (and "m_scale", "v_scale"), made here as zeros when not given; state_lists()
+    returns it, which with `steps` is what a checkpoint has to keep.  decay: one truth value per tensor.  seed: names the random
+    bits by which 8-bit codes are rounded."""
+
+    def __init__(self, params, grads, bits: int = 32, state=None, decay=None, steps: int = 0, seed: int = 0):
+        import torch
+        params, grads = list(params), list(grads)
+        _invalid("bits is 8 or 32", bits in (8, 32))
+        _invalid("one gradient per parameter", len(params) == len(grads))
+        decay = [True] * len(params) if decay is None else list(decay)
+        _invalid("one truth value of decay per parameter", len(decay) == len(params))
+        blocks = [(p.numel() + 255) // 256 for p in params]
+        if state is None:
+            held = torch.float32 if bits == 32 else torch.float8_e4m3fn
+            zeros = lambda n, p, t: torch.zeros(n, dtype=torch.uint8 if t.itemsize == 1 else t, device=p.device).view(t)  # noqa: E731
+            state = {k: [zeros(p.numel(), p, held) for p in params] for k in ("m", "v")}
+            if bits == 8:
+                state.update({k: [zeros(b, p, torch.float32) for p, b in zip(params, blocks)] for k in ("m_scale", "v_scale")})
+        names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
+        _invalid(f"state has the lists {names}", sorted(state) == sorted(names) and all(len(state[k]) == len(params) for k in names))
+        self.device = params[0].device if params else None
+        spans = []
+        for i, (p, g, b) in enumerate(zip(params, grads, blocks)):
+            _invalid(f"tensor {i}: gradient of the parameter's shape", p.shape == g.shape)
+            parts = [(p, None, p.numel()), (g, None, p.numel())]
+            held = torch.float32 if bits == 32 else torch.float8_e4m3fn
+            parts += [(state[k][i], held, p.numel()) for k in ("m", "v")]
+            parts += [(state[k][i], torch.float32, b) for k in names[2:]]
+            for j, (t, want, n) in enumerate(parts):
+                _invalid(f"tensor {i}: contiguous tensors on {self.device}", t.is_cuda and t.device == self.device and t.is_contiguous())
+                _invalid(f"tensor {i}: {n} elements of moments, {b} constants, of their types", t.numel() == n and want in (None, t.dtype))
+                if n:
+                    spans.append((t.data_ptr(), t.data_ptr() + n * t.element_size(), j != 1))
+        # what is written may overlap nothing else
+        spans.sort()
+        end, end_w = 0, 0
+        for a, b, w in spans:
+            _invalid("no two of the tensors overlap", a >= (end if w else end_w))
+            end, end_w = max(end, b), max(end_w, b if w else 0)
+        self._keep = (params, grads, state)
+        self.bits, self.steps, self.seed, self._state = bits, int(steps), int(seed) & 0xFFFFFFFF, state
+        self._list = (_AdamWTensor * max(1, len(params)))()
+        for i, (p, g) in enumerate(zip(params, grads)):
+            at = [state[k][i].data_ptr() if k in state else None for k in ("m", "v", "m_scale", "v_scale")]
+            self._list[i] = _AdamWTensor(p.data_ptr(), g.data_ptr(), *at, p.numel(), _dtype(p.dtype), _dtype(g.dtype), int(bool(decay[i])))
+        self._count = len(params)
+
+    def state_lists(self):
+        return self._state
+
+    def step(self, hp: AdamW, grad_scale: float = 1.0, step=None):
+        """One update.  step: None counts on from `steps`; a CUDA int64 tensor of one element holds the number of the step on the
+        device (from 1; the caller moves it on), which a step captured into a graph needs."""
+        import torch
+        if self._count == 0:
+            return
+        dev = None
+        if step is not None:
+            _invalid("step is a CUDA int64 tensor of one element", torch.is_tensor(step) and step.device == self.device and step.dtype == torch.int64
+                     and step.numel() == 1)
+            dev = step.data_ptr()
+        st = load_library().pac_adamw_tensors(self.device.index, _stream(self.device), self._list, self._count, self.bits, C.byref(hp._c()), self.steps + 1, dev,
+                                              grad_scale, self.seed)
+        if st != 0:
+            raise PacError(st, "pac_adamw_tensors failed" + (": under capture the step's number has to be on the device" if st == 2 else ""))
+        if dev is None:
+            self.steps += 1

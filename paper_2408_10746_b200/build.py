@@ -9,12 +9,14 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libpac_b200.so")
-SOURCES = [os.path.join(HERE, "csrc", "pac_api.cu")]
-HEADERS = [os.path.join(HERE, "csrc", f) for f in ("pac_common.cuh", "pac_simt.cuh", "pac_tensor.cuh", "pac_mid.cuh", "pac_fused_fwd.cuh", "pac_gemm.cuh", "pac_quant.cuh", "pac_chain_fwd.cuh", "pac_tbody.cuh", "pac_xgemm.cuh", "pac_tbody_fused.cuh")] + \
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("pac_api.cu", "pac_lowbit_api.cu")]
+HEADERS = [os.path.join(HERE, "csrc", f) for f in ("pac_common.cuh", "pac_simt.cuh", "pac_tensor.cuh", "pac_mid.cuh", "pac_fused_fwd.cuh", "pac_gemm.cuh", "pac_quant.cuh", "pac_chain_fwd.cuh", "pac_tbody.cuh", "pac_xgemm.cuh", "pac_tbody_fused.cuh",
+                                                   "pac_ptx.cuh", "pac_adamw.cuh", "pac_adamw_tensors.cuh", "pac_mxfp.cuh", "pac_mxfp_linear.cuh", "pac_mxfp_product.cuh")] + \
           [os.path.join(ROOT, "include", "pac.h")]
 
 
@@ -29,17 +31,24 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
-           "-I", os.path.join(HERE, "csrc"), "-o", LIB] + SOURCES
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
+             "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        flags = ["-Xptxas", "-v"] + flags
+    with tempfile.TemporaryDirectory() as tmp:
+        # one compiler per source, side by side
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        running = [subprocess.Popen([nvcc, *flags, "-c", src, "-o", obj], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+                   for src, obj in zip(SOURCES, objects)]
+        said = [p.communicate()[0] for p in running]
+        for p, out in zip(running, said):
+            if p.returncode != 0:
+                raise RuntimeError("nvcc failed:\n" + out)
+        res = subprocess.run([nvcc, *flags, "-shared", "-o", LIB, *objects], capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
     if verbose:
-        print(res.stderr)
+        print("".join(said))
     return LIB
 
 

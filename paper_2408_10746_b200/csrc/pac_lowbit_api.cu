@@ -1,0 +1,267 @@
+// C entries of what a trainer keeps in few bits: the MXFP4 codec and its products, and the AdamW step over a list of
+// tensors.  None of them allocates device memory or keeps anything from call to call; all work is enqueued on the
+// caller's stream and may be captured.
+#include <cmath>
+
+#include "pac_adamw_tensors.cuh"
+#include "pac_mxfp.cuh"
+#include "pac_mxfp_linear.cuh"
+#include "pac_mxfp_product.cuh"
+
+using namespace pac;
+
+namespace {
+
+// Makes `device` current for the length of a call.
+struct OnDevice {
+    int prev = -1;
+    bool ok = false;
+    explicit OnDevice(int device) {
+        int cur = -1;
+        if (cudaGetDevice(&cur) != cudaSuccess) { cudaGetLastError(); return; }
+        if (cur == device) { ok = true; return; }
+        if (cudaSetDevice(device) != cudaSuccess) { cudaGetLastError(); return; }
+        prev = cur;
+        ok = true;
+    }
+    ~OnDevice() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+bool dtype_ok(int t) { return t == PAC_F32 || t == PAC_BF16; }
+size_t dtype_size(int t) { return t == PAC_F32 ? 4 : 2; }
+
+int sm_count(int device) {
+    int n = 0;
+    return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) == cudaSuccess && n > 0 ? n : 148;
+}
+pac_status launched() { return cudaGetLastError() == cudaSuccess ? PAC_OK : PAC_ERR_CUDA; }
+
+// [rows][inner] array of `type` elements with a row pitch in bytes, boxes of box_inner x box_rows; elements outside read as 0.
+bool map_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, long long inner, long long rows, long long pitch, int box_inner, int box_rows,
+            CUtensorMapSwizzle swizzle) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+    return fn(map, type, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Sizes that every call on an MXFP4 matrix checks: rows and columns, and tile coordinates that fit 32 bits.
+bool matrix_ok(const void* codes, const void* scales, long long rows, int cols) {
+    return codes && scales && aligned(codes, 16) && aligned(scales, 16) && rows >= 1 && rows <= 0x7fffff00LL && cols >= 1 && cols <= 0x7fffff00;
+}
+
+cudaError_t opt_in(const void* kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
+
+template <bool GRAD, int XMODE>
+cudaError_t launch_linear(cudaStream_t st, const CUtensorMap& codes, const CUtensorMap& x, const MlParams& p) {
+    const auto kernel = mxfp_linear_kernel<GRAD, XMODE>;
+    const size_t smem = 1024 + p.code_at + (size_t)p.code_stages * ML_CODE_BYTES;
+    cudaError_t e = opt_in((const void*)kernel, smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(((p.o.cols + 127LL) / 128) * p.o.split), (unsigned)((p.o.M + p.o.nt - 1) / p.o.nt));
+    cfg.blockDim = dim3(XMODE == ML_X_TMA ? 320 : 448);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.o.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.o.split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, codes, x, p);
+}
+
+pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x_dtype, int M, long long ldx, const unsigned char* codes,
+                       const unsigned char* scales, int N, int K, void* y, int y_dtype, long long ldy) {
+    const int red = grad ? N : K, out_cols = grad ? K : N;
+    if (M < 0 || !matrix_ok(codes, scales, N, K) || !dtype_ok(x_dtype) || !dtype_ok(y_dtype)) return PAC_ERR_INVALID_ARG;
+    if (M == 0) return PAC_OK;
+    if (!x || !y || ldx < red || ldy < out_cols || M > 0x7fffff00) return PAC_ERR_INVALID_ARG;
+    if (!aligned(x, dtype_size(x_dtype)) || !aligned(y, dtype_size(y_dtype))) return PAC_ERR_INVALID_ARG;
+    OnDevice on(device);
+    if (!on.ok) return PAC_ERR_CUDA;
+    MlParams p = {};
+    p.x = x; p.ldx = ldx; p.scales = scales; p.o.y = y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32;
+    p.o.M = M; p.o.cols = out_cols; p.red = red; p.pieces = mx_col_pieces(K);
+    const bool rows16 = aligned(x, 16) && (ldx * (long long)dtype_size(x_dtype)) % 16 == 0;
+    const int mode = x_dtype == PAC_F32 ? ML_X_F32 : rows16 ? ML_X_TMA : ML_X_BF16;
+    p.x_vec = rows16;
+    if (!ml_plan(p, mode == ML_X_F32, mode != ML_X_TMA, sm_count(device))) return PAC_ERR_UNSUPPORTED;
+    CUtensorMap mc, mx;
+    if (!map_2d(&mc, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, mx_row_bytes(K), N, mx_row_bytes(K), 64, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) return PAC_ERR_CUDA;
+    mx = mc;
+    if (mode == ML_X_TMA && !map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, red, M, ldx * 2, ML_BK, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B)) return PAC_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e;
+    if (grad)
+        e = mode == ML_X_TMA ? launch_linear<true, ML_X_TMA>(st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<true, ML_X_BF16>(st, mc, mx, p)
+                                                                                                 : launch_linear<true, ML_X_F32>(st, mc, mx, p);
+    else
+        e = mode == ML_X_TMA ? launch_linear<false, ML_X_TMA>(st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<false, ML_X_BF16>(st, mc, mx, p)
+                                                                                                  : launch_linear<false, ML_X_F32>(st, mc, mx, p);
+    if (e != cudaSuccess) { cudaGetLastError(); return PAC_ERR_CUDA; }
+    return PAC_OK;
+}
+
+}  // namespace
+
+extern "C" pac_status pac_quantize_mxfp(int device, void* cuda_stream, const void* dev_x, int dtype, long long rows, int cols, long long ldx,
+                                        unsigned char* dev_codes, unsigned char* dev_scales) {
+    if (rows < 0 || !dtype_ok(dtype) || cols < 1) return PAC_ERR_INVALID_ARG;
+    if (rows == 0) return PAC_OK;
+    if (!dev_x || !aligned(dev_x, dtype_size(dtype)) || ldx < cols || !matrix_ok(dev_codes, dev_scales, rows, cols)) return PAC_ERR_INVALID_ARG;
+    OnDevice on(device);
+    if (!on.ok) return PAC_ERR_CUDA;
+    const bool vec = aligned(dev_x, 32) && (ldx * (long long)dtype_size(dtype)) % 32 == 0;
+    const long long items = (rows + MX_TILE - 1) / MX_TILE * (MX_TILE / 4) * (mx_col_pieces(cols) / 2);
+    const long long want = (items + 7) / 8, most = 148LL * 32;
+    const unsigned grid = (unsigned)(want < most ? want : most);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == PAC_F32) quantize_mxfp_kernel<float><<<grid, 256, 0, st>>>((const float*)dev_x, rows, cols, ldx, vec, dev_codes, dev_scales);
+    else quantize_mxfp_kernel<bf16><<<grid, 256, 0, st>>>((const bf16*)dev_x, rows, cols, ldx, vec, dev_codes, dev_scales);
+    return launched();
+}
+
+extern "C" pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const unsigned char* dev_codes, const unsigned char* dev_scales, long long rows,
+                                          int cols, void* dev_out, int dtype, long long ldo) {
+    if (rows < 0 || !dtype_ok(dtype) || cols < 1) return PAC_ERR_INVALID_ARG;
+    if (rows == 0) return PAC_OK;
+    if (!dev_out || !aligned(dev_out, dtype_size(dtype)) || ldo < cols || !matrix_ok(dev_codes, dev_scales, rows, cols)) return PAC_ERR_INVALID_ARG;
+    OnDevice on(device);
+    if (!on.ok) return PAC_ERR_CUDA;
+    const bool vec = aligned(dev_out, 32) && (ldo * (long long)dtype_size(dtype)) % 32 == 0;
+    const long long want = (rows * (mx_row_bytes(cols) / 8) + 255) / 256, most = 148LL * 32;
+    const unsigned grid = (unsigned)(want < most ? want : most);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == PAC_F32) dequantize_mxfp_kernel<float><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (float*)dev_out, ldo, vec);
+    else dequantize_mxfp_kernel<bf16><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (bf16*)dev_out, ldo, vec);
+    return launched();
+}
+
+extern "C" pac_status pac_mxfp_linear(int device, void* cuda_stream, const void* dev_x, int x_dtype, int M, long long ldx, const unsigned char* dev_codes,
+                                      const unsigned char* dev_scales, int N, int K, void* dev_y, int y_dtype, long long ldy) {
+    return mxfp_linear(false, device, cuda_stream, dev_x, x_dtype, M, ldx, dev_codes, dev_scales, N, K, dev_y, y_dtype, ldy);
+}
+
+extern "C" pac_status pac_mxfp_linear_grad(int device, void* cuda_stream, const void* dev_dy, int dy_dtype, int M, long long lddy,
+                                           const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_dx, int dx_dtype,
+                                           long long lddx) {
+    return mxfp_linear(true, device, cuda_stream, dev_dy, dy_dtype, M, lddy, dev_codes, dev_scales, N, K, dev_dx, dx_dtype, lddx);
+}
+
+extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsigned char* dev_a_codes, const unsigned char* dev_a_scales, int M,
+                                       const unsigned char* dev_b_codes, const unsigned char* dev_b_scales, int N, int K, void* dev_y, int y_dtype,
+                                       long long ldy) {
+    if (M < 0 || !matrix_ok(dev_b_codes, dev_b_scales, N, K) || !dtype_ok(y_dtype)) return PAC_ERR_INVALID_ARG;
+    if (M == 0) return PAC_OK;
+    if (!matrix_ok(dev_a_codes, dev_a_scales, M, K) || !dev_y || !aligned(dev_y, dtype_size(y_dtype)) || ldy < N) return PAC_ERR_INVALID_ARG;
+    OnDevice on(device);
+    if (!on.ok) return PAC_ERR_CUDA;
+    MpParams p = {};
+    p.a_scales = dev_a_scales; p.b_scales = dev_b_scales;
+    p.o.y = dev_y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32; p.o.M = M; p.o.cols = N;
+    p.pieces = mx_col_pieces(K);
+    if (!mp_plan(p, K, sm_count(device))) return PAC_ERR_UNSUPPORTED;
+    CUtensorMap ma, mb;
+    if (!map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, dev_a_codes, mx_row_bytes(K), M, mx_row_bytes(K), 128, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, dev_b_codes, mx_row_bytes(K), N, mx_row_bytes(K), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))
+        return PAC_ERR_CUDA;
+    const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes;
+    cudaError_t e = opt_in((const void*)mxfp_product_kernel, smem);
+    if (e == cudaSuccess) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(((N + 127LL) / 128) * p.o.split), (unsigned)((M + p.o.nt - 1) / p.o.nt));
+        cfg.blockDim = dim3(320);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = (cudaStream_t)cuda_stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)p.o.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = p.o.split > 1 ? 1 : 0;
+        e = cudaLaunchKernelEx(&cfg, mxfp_product_kernel, ma, mb, p);
+    }
+    if (e != cudaSuccess) { cudaGetLastError(); return PAC_ERR_CUDA; }
+    return PAC_OK;
+}
+
+// ---------------------------------------------------------------------------
+// AdamW over a list of tensors
+// ---------------------------------------------------------------------------
+namespace {
+
+template <int BITS, int CAP>
+cudaError_t launch_adamw(cudaStream_t st, const pac_adamw_tensor* t, int count, AtStep s, int sms) {
+    AtList<CAP> list;
+    unsigned long long blocks = 0;
+    for (int i = 0; i < count; ++i) {
+        AtTensor& a = list.t[i];
+        a.p = t[i].p; a.g = t[i].g; a.m = t[i].m; a.v = t[i].v; a.m_scale = t[i].m_scale; a.v_scale = t[i].v_scale; a.n = t[i].n;
+        a.first_block = (uint32_t)blocks;
+        const size_t pa = t[i].p_dtype == PAC_F32 ? 32 : 16, ga = t[i].g_dtype == PAC_F32 ? 32 : 16, sa = BITS == 32 ? 32 : 8;
+        const bool vec = aligned(a.p, pa) && aligned(a.g, ga) && aligned(a.m, sa) && aligned(a.v, sa);
+        a.flags = (t[i].p_dtype == PAC_BF16 ? AT_P16 : 0u) | (t[i].g_dtype == PAC_BF16 ? AT_G16 : 0u) | (t[i].decay ? AT_DECAY : 0u) | (vec ? AT_VEC : 0u);
+        blocks += (unsigned long long)((t[i].n + AT_BLOCK - 1) / AT_BLOCK);
+    }
+    s.count = count;
+    s.blocks = (uint32_t)blocks;
+    const unsigned long long want = (blocks + 7) / 8, most = (unsigned long long)sms * 32;
+    adamw_tensors_kernel<BITS, CAP><<<(unsigned)(want < most ? want : most), 256, 0, st>>>(list, s);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+extern "C" pac_status pac_adamw_tensors(int device, void* cuda_stream, const pac_adamw_tensor* tensors, int count, int state_bits, const pac_adamw* hp,
+                                        long long step, const long long* dev_step, float grad_scale, unsigned seed) {
+    if (count < 0 || !hp || (state_bits != 8 && state_bits != 32) || (count > 0 && !tensors) || (!dev_step && step < 1)) return PAC_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i) {
+        const pac_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > (1LL << 39) || !dtype_ok(t.p_dtype) || !dtype_ok(t.g_dtype)) return PAC_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (!t.p || !t.g || !t.m || !t.v || !aligned(t.p, dtype_size(t.p_dtype)) || !aligned(t.g, dtype_size(t.g_dtype))) return PAC_ERR_INVALID_ARG;
+        if (state_bits == 32 && (!aligned(t.m, 4) || !aligned(t.v, 4))) return PAC_ERR_INVALID_ARG;
+        if (state_bits == 8 && (!t.m_scale || !t.v_scale || !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))) return PAC_ERR_INVALID_ARG;
+    }
+    OnDevice on(device);
+    if (!on.ok) return PAC_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (!dev_step) {
+        // a replayed graph would take this very step again and again
+        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) { cudaGetLastError(); return PAC_ERR_CUDA; }
+        if (cap != cudaStreamCaptureStatusNone) return PAC_ERR_BAD_STATE;
+    }
+    AtStep s = {};
+    s.hp = *hp; s.grad_scale = grad_scale; s.seed = seed; s.dev_step = dev_step;
+    if (!dev_step) {
+        s.step = (uint32_t)step;
+        s.bc1 = (float)(1.0 - std::pow((double)hp->beta1, (double)step));
+        s.bc2 = (float)(1.0 - std::pow((double)hp->beta2, (double)step));
+    }
+    const int sms = sm_count(device);
+    for (int at = 0; at < count;) {
+        // as many tensors as a list holds and whose blocks a 32-bit number counts; empty tensors only end a run
+        int n = 0;
+        unsigned long long blocks = 0;
+        while (at < count && tensors[at].n == 0) ++at;
+        const int most = count - at <= AT_SMALL ? AT_SMALL : AT_LARGE;
+        while (at + n < count && n < most && tensors[at + n].n > 0) {
+            const unsigned long long b = (unsigned long long)((tensors[at + n].n + AT_BLOCK - 1) / AT_BLOCK);
+            if (blocks + b > 0x7fffffffULL && n > 0) break;
+            blocks += b;
+            ++n;
+        }
+        if (n == 0) break;
+        s.first_tensor = at;
+        cudaError_t e;
+        if (n <= AT_SMALL) e = state_bits == 8 ? launch_adamw<8, AT_SMALL>(st, tensors + at, n, s, sms) : launch_adamw<32, AT_SMALL>(st, tensors + at, n, s, sms);
+        else e = state_bits == 8 ? launch_adamw<8, AT_LARGE>(st, tensors + at, n, s, sms) : launch_adamw<32, AT_LARGE>(st, tensors + at, n, s, sms);
+        if (e != cudaSuccess) return PAC_ERR_CUDA;
+        at += n;
+    }
+    return PAC_OK;
+}

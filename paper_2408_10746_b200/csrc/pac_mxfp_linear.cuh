@@ -1,0 +1,401 @@
+// Products with a frozen matrix W [N][K] in MXFP4 (pac_mxfp.cuh), the other operand as it is:
+//     y  = x W^T      [M][N]      (GRAD = false; reduction over the columns of W)
+//     dx = dy W       [M][K]      (GRAD = true;  reduction over the rows of W; W is frozen, so this is the whole backward pass)
+//
+// A value of W is a bf16 exactly (two significant bits times a power of two), so W goes through the bf16 tensor cores
+// without an error of its own: converter warps turn codes into a bf16 tile in shared memory, tcgen05.mma takes it from
+// there.  W is the M operand (128 of its rows, or of its columns, per CTA) and the tokens are the N operand: few tokens
+// cost few columns, each code is converted once per CTA however many tokens there are, and in the accumulator a lane is
+// an output column, so that a warp's store is 32 neighbours of a row of y without a detour through shared memory.
+//
+// Both directions walk W in pieces of 128 rows x 128 columns: 8 KB of codes and 512 bytes of scales, two K steps of 64.
+// Forward the tile is K-major (a thread converts one block of 32 of a row), backward MN-major (the same block lies along
+// the M dimension): the same 64 bytes go to another place, and the descriptor says so.
+//
+// Few tiles: the reduction is split over a cluster, whose CTAs then add their partial sums through distributed shared
+// memory in the order of their ranks (no atomics, no workspace).
+//
+// Precision: operands exact, sums in fp32.  The tensor core cuts partial sums instead of rounding them, so K steps take
+// turns over the accumulators that tensor memory has room for.  x in fp32 enters as three bf16 terms that add up to it
+// exactly; the second and third share an accumulator.
+#pragma once
+#include <cooperative_groups.h>
+#include <type_traits>
+
+#include "pac_mxfp.cuh"
+
+namespace pac {
+
+constexpr int ML_BK = 64;                                   // reduction elements per stage
+constexpr int ML_CONV_WARPS = 8, ML_X_WARPS = 4;
+constexpr uint32_t ML_A_BYTES = 128 * ML_BK * 2;
+constexpr uint32_t ML_CODE_BYTES = 128 * 64 + MX_SCALE_PIECE;
+constexpr int ML_MAX_STAGES = 8, ML_MAX_CODES = 8;
+constexpr size_t ML_SMEM_MOST = 232448 - 1024 - 512;
+enum { ML_X_TMA = 0, ML_X_BF16 = 1, ML_X_F32 = 2 };         // how x reaches shared memory: TMA boxes, or threads (any alignment, or fp32)
+
+// What becomes of a product's accumulators (the block-scaled product's as well).
+struct MxOut {
+    void* y; long long ldy; int y_f32;
+    int M;                                                  // tokens
+    int cols;                                               // columns of y
+    int nt;                                                 // tokens per tile, a multiple of 16
+    int split;                                              // CTAs of a cluster that share a tile's reduction
+    int n_acc;                                              // accumulators of nt columns
+};
+struct MlParams {
+    MxOut o;
+    const void* x; long long ldx;                           // ML_X_BF16, ML_X_F32
+    const unsigned char* scales;
+    int red;                                                // length of the reduction: K, or N with GRAD
+    int pieces;                                             // pieces of scales per row tile
+    int red_tiles;                                          // ceil(red / 128)
+    int stages, code_stages;
+    uint32_t stage_bytes, code_at;                          // bytes per stage; offset of the ring of codes
+    uint32_t tmem_cols;
+    bool x_vec;                                             // rows of x start on 16-byte boundaries
+};
+
+__device__ __forceinline__ void ml_tma_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v) { asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// Accumulators -> y, by all threads of the CTA.  A lane is an output column and an accumulator column a token, so a warp
+// stores 32 neighbours of a row of y; warps 2-9, two per quadrant of lanes, share the tokens.  A tile whose reduction is
+// split goes through shared memory and is added up by the cluster, rank by rank.  `used`: accumulators that some step has
+// written; `last`: the last one has been written in any case.
+__device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, unsigned char* smem, uint32_t accf, volatile int* abort_flag, int wt, int t0,
+                                          int rank, int used, bool last) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n_tok = min(o.nt, o.M - t0);
+    if (warp >= 2 && warp < 10) {
+        const bool ok = mbar_wait_uniform(accf, 0, abort_flag, nullptr);
+        if (!ok) drain_after_abort(abort_flag);              // copies in flight land before their memory is written again
+        tc_fence_after();
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const int col = wt * 128 + q * 32 + lane;
+        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16);
+        float* part = reinterpret_cast<float*>(smem);
+        const float bad = __uint_as_float(0x7fffffffu);      // a wait that ran out leaves NaN, not a wrong number
+        for (int c0 = half * 16; c0 < o.nt; c0 += 32) {
+            float v[16];
+            tmem_ld16(taddr + c0, v);
+            tmem_ld_wait();
+            for (int a = 1; a < o.n_acc; ++a) {
+                if (a >= used && !(last && a == o.n_acc - 1)) continue;
+                float w[16];
+                tmem_ld16(taddr + a * o.nt + c0, w);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] += w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (!ok) v[e] = bad;
+                if (o.split > 1) {
+                    part[(c0 + e) * 128 + q * 32 + lane] = v[e];
+                } else if (c0 + e < n_tok && col < o.cols) {
+                    const long long at = (long long)(t0 + c0 + e) * o.ldy + col;
+                    if (o.y_f32) static_cast<float*>(o.y)[at] = v[e];
+                    else static_cast<bf16*>(o.y)[at] = __float2bfloat16(v[e]);
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (o.split > 1) {
+        namespace cg = cooperative_groups;
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        const float* part = reinterpret_cast<const float*>(smem);
+        const int threads = (int)blockDim.x;
+        // tokens in turn over the ranks
+        const int mine = rank < n_tok ? (n_tok - rank + o.split - 1) / o.split : 0;
+        for (int i = threadIdx.x; i < mine * 128; i += threads) {
+            const int c = (i >> 7) * o.split + rank, n = i & 127, col = wt * 128 + n;
+            float v = 0.f;
+            for (int k = 0; k < o.split; ++k) v += cluster.map_shared_rank(part, k)[c * 128 + n];
+            if (col < o.cols) {
+                const long long at = (long long)(t0 + c) * o.ldy + col;
+                if (o.y_f32) static_cast<float*>(o.y)[at] = v;
+                else static_cast<bf16*>(o.y)[at] = __float2bfloat16(v);
+            }
+        }
+        cluster.sync();                                      // nobody leaves while its partial sums are still read
+    }
+}
+
+// Eight values of a row of x from element `at` on (0 where `have` runs out).
+__device__ __forceinline__ void ml_load8(const bf16* p, bool vec, int have, uint4& u) {
+    if (vec && have >= 8) { u = *reinterpret_cast<const uint4*>(p); return; }
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < have) w[e >> 1] |= (uint32_t)__bfloat16_as_ushort(p[e]) << (16 * (e & 1));
+    u = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void ml_load8(const float* p, bool vec, int have, float4 (&u)[2]) {
+    if (vec && have >= 8) { u[0] = *reinterpret_cast<const float4*>(p); u[1] = *reinterpret_cast<const float4*>(p + 4); return; }
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = e < have ? p[e] : 0.f;
+    u[0] = make_float4(f[0], f[1], f[2], f[3]); u[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+
+// Warps: 0 copies, 1 MMAs, 2-9 convert W and store y, 10-13 (not ML_X_TMA) bring in x.
+template <bool GRAD, int XMODE>
+__global__ void __launch_bounds__(XMODE == ML_X_TMA ? 320 : 448, 1)
+mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x, const MlParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    constexpr int TERMS = XMODE == ML_X_F32 ? 3 : 1;
+    __shared__ __align__(8) unsigned long long bars[3 * ML_MAX_STAGES + 2 * ML_MAX_CODES + 1];
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ int abort_sh;
+    const uint32_t xfull0 = smem_u32(&bars[0]), afull0 = smem_u32(&bars[ML_MAX_STAGES]), empty0 = smem_u32(&bars[2 * ML_MAX_STAGES]);
+    const uint32_t cfull0 = smem_u32(&bars[3 * ML_MAX_STAGES]), cempty0 = smem_u32(&bars[3 * ML_MAX_STAGES + ML_MAX_CODES]);
+    const uint32_t accf = smem_u32(&bars[3 * ML_MAX_STAGES + 2 * ML_MAX_CODES]);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = p.o.split > 1 ? (int)(blockIdx.x % p.o.split) : 0;
+    const int wt = blockIdx.x / p.o.split, t0 = blockIdx.y * p.o.nt;
+    const int kt0 = (int)((long long)p.red_tiles * rank / p.o.split), kt1 = (int)((long long)p.red_tiles * (rank + 1) / p.o.split);
+    const uint32_t ring0 = smem_u32(smem), codes0 = ring0 + p.code_at;
+    const uint32_t term_bytes = (uint32_t)p.o.nt * 128u;
+
+    if (threadIdx.x == 0) {
+        abort_sh = 0;
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(xfull0 + 8 * s, XMODE == ML_X_TMA ? 1 : ML_X_WARPS);
+            mbar_init(afull0 + 8 * s, ML_CONV_WARPS);
+            mbar_init(empty0 + 8 * s, 1);
+        }
+        for (int s = 0; s < p.code_stages; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, ML_CONV_WARPS); }
+        mbar_init(accf, 1);
+        fence_mbar_init();
+        tma_prefetch_desc(&map_codes);
+        if (XMODE == ML_X_TMA) tma_prefetch_desc(&map_x);
+    }
+    if (warp == 1) { tmem_alloc(smem_u32(&tmem_base_sh), p.tmem_cols); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_base_sh;
+    volatile int* abort_flag = &abort_sh;
+
+    if (warp == 0) {
+        uint32_t cs = 0, cph = 1, s = 0, ph = 1;             // parities of the "free" phases to wait for
+        bool ok = true;
+        for (int kt = kt0; kt < kt1 && ok; ++kt) {
+            ok = mbar_wait_uniform(cempty0 + 8 * cs, cph, abort_flag, nullptr);
+            if (!ok) break;
+            if (elect_one()) {
+                const uint32_t bar = cfull0 + 8 * cs, dst = codes0 + cs * ML_CODE_BYTES;
+                mbar_expect_tx(bar, ML_CODE_BYTES);
+                const long long rt = GRAD ? kt : wt, ct = GRAD ? wt : kt;
+                ml_tma_2d(dst, &map_codes, bar, (int)ct * 64, (int)rt * 128);
+                bulk_load_1d(dst + 128 * 64, p.scales + (rt * p.pieces + ct) * (long long)MX_SCALE_PIECE, MX_SCALE_PIECE, bar);
+            }
+            __syncwarp();
+            if (++cs == (uint32_t)p.code_stages) { cs = 0; cph ^= 1u; }
+            if constexpr (XMODE == ML_X_TMA) {
+                for (int h = 0; h < 2 && ok; ++h) {
+                    ok = mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        mbar_expect_tx(xfull0 + 8 * s, term_bytes);
+                        ml_tma_2d(ring0 + s * p.stage_bytes + ML_A_BYTES, &map_x, xfull0 + 8 * s, kt * 128 + h * 64, t0);
+                    }
+                    __syncwarp();
+                    if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        const uint32_t idesc = instr_desc_bf16(128, p.o.nt, GRAD ? 1 : 0, 0);
+        const uint64_t a0 = GRAD ? smem_desc_sw128(ring0, 8192, 1024) : smem_desc_sw128(ring0, 16, 1024);
+        const uint64_t b0 = smem_desc_sw128(ring0 + ML_A_BYTES, 16, 1024);
+        const uint64_t astep = GRAD ? 128u : 2u;             // 16 elements of the reduction further, in 16-byte units
+        uint32_t s = 0, ph = 0, acc = 0;
+        const int steps = 2 * (kt1 - kt0), lead = TERMS == 1 ? p.o.n_acc : p.o.n_acc - 1;
+        bool ok = true;
+        for (int i = 0; i < steps && ok; ++i) {
+            ok = mbar_wait_uniform(xfull0 + 8 * s, ph, abort_flag, nullptr) && mbar_wait_uniform(afull0 + 8 * s, ph, abort_flag, nullptr);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
+#pragma unroll
+                for (int k = 0; k < ML_BK / 16; ++k)
+                    umma_bf16(tmem_base + acc * p.o.nt, a0 + off + astep * k, b0 + off + 2 * k, idesc, (i >= lead || k) ? 1u : 0u);
+                if constexpr (TERMS == 3) {
+                    const uint64_t tb = term_bytes >> 4;
+#pragma unroll
+                    for (int t = 1; t < 3; ++t)
+#pragma unroll
+                        for (int k = 0; k < ML_BK / 16; ++k)
+                            umma_bf16(tmem_base + lead * p.o.nt, a0 + off + astep * k, b0 + off + t * tb + 2 * k, idesc, (i | k | (t - 1)) ? 1u : 0u);
+                }
+                umma_commit(empty0 + 8 * s);
+            }
+            __syncwarp();
+            if (++acc == (uint32_t)lead) acc = 0;
+            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+        }
+        if (elect_one()) umma_commit(accf);
+        __syncwarp();
+    } else if (warp < 2 + ML_CONV_WARPS) {
+        const int t = threadIdx.x - 64;
+        uint32_t cs = 0, cph = 0, s = 0, ph = 1;
+        bool ok = true;
+        // this thread's block of 32: forward row t / 2, block t % 2 of the step's 64 columns; backward row t / 4 of the
+        // step's 64 rows, block t % 4 of the 128 columns
+        const int r = GRAD ? t >> 2 : t >> 1, b = GRAD ? t & 3 : t & 1;
+        const uint32_t dst0 = GRAD ? (uint32_t)((b >> 1) * 8192 + r * 128) : (uint32_t)(r * 128);
+        const uint32_t chunk0 = GRAD ? (uint32_t)(b & 1) * 4u : (uint32_t)b * 4u, swz = (uint32_t)r & 7u;
+        for (int kt = kt0; kt < kt1 && ok; ++kt) {
+            ok = mbar_wait_uniform(cfull0 + 8 * cs, cph, abort_flag, nullptr);
+            if (!ok) break;
+            const uint32_t src = codes0 + cs * ML_CODE_BYTES;
+            uint4 c[2];
+            uint32_t f[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = GRAD ? h * 64 + r : r, blk = GRAD ? b : h * 2 + b;
+                c[h] = lds128(src + row * 64 + blk * 16);
+                // beyond the reduction the codes are 0 and the scale is whatever fills the piece: it must not be a NaN
+                const bool in = GRAD ? kt * 128 + row < p.red : kt * 128 + blk * 32 < p.red;
+                f[h] = in ? mx_scale_bf16x2(lds8(src + 128 * 64 + mx_scale_at((uint32_t)row, (uint32_t)blk))) : 0u;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(cempty0 + 8 * cs);
+            if (++cs == (uint32_t)p.code_stages) { cs = 0; cph ^= 1u; }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t o[4][4];
+                const uint32_t w[4] = {c[h].x, c[h].y, c[h].z, c[h].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    mx_bf16x8(w[j], o[j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[j][e] = mul_bf16x2(o[j][e], f[h]);
+                }
+                ok = ok && mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr);
+                if (!ok) break;
+                const uint32_t dst = ring0 + s * p.stage_bytes + dst0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sts128(dst + ((chunk0 + j) ^ swz) * 16u, make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]));
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(afull0 + 8 * s);
+                if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+            }
+        }
+    } else {
+        // x by threads: 16-byte chunks of the swizzled tile, the next step's values on their way while this step waits for its stage
+        const int t = threadIdx.x - 64 - 32 * ML_CONV_WARPS;
+        constexpr int PER = XMODE == ML_X_F32 ? 4 : 8;       // chunks per thread: 64 tokens (fp32), 128 tokens
+        typedef typename std::conditional<XMODE == ML_X_F32, float, bf16>::type T;
+        uint32_t s = 0, ph = 1;
+        const int steps = 2 * (kt1 - kt0), chunks = p.o.nt * 8;
+        uint4 nb[PER];
+        float4 nf[PER][2];
+        auto fetch = [&](int i) {
+            const int k0 = kt0 * 128 + i * 64;
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                const int id = q * 128 + t, row = t0 + (id >> 3), at = k0 + (id & 7) * 8;
+                const int have = (id < chunks && row < p.o.M) ? p.red - at : 0;
+                const T* src = static_cast<const T*>(p.x) + (long long)row * p.ldx + at;
+                if constexpr (XMODE == ML_X_F32) {
+                    if (have > 0) ml_load8(src, p.x_vec, have, nf[q]);
+                    else nf[q][0] = nf[q][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+                } else {
+                    if (have > 0) ml_load8(src, p.x_vec, have, nb[q]);
+                    else nb[q] = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
+        };
+        if (steps > 0) fetch(0);
+        for (int i = 0; i < steps; ++i) {
+            uint4 u[PER][TERMS];
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                if constexpr (XMODE == ML_X_F32) {
+                    uint32_t h[4], m[4], l[4];
+                    split3_pair(nf[q][0].x, nf[q][0].y, h[0], m[0], l[0]);
+                    split3_pair(nf[q][0].z, nf[q][0].w, h[1], m[1], l[1]);
+                    split3_pair(nf[q][1].x, nf[q][1].y, h[2], m[2], l[2]);
+                    split3_pair(nf[q][1].z, nf[q][1].w, h[3], m[3], l[3]);
+                    u[q][0] = make_uint4(h[0], h[1], h[2], h[3]);
+                    u[q][1] = make_uint4(m[0], m[1], m[2], m[3]);
+                    u[q][2] = make_uint4(l[0], l[1], l[2], l[3]);
+                } else {
+                    u[q][0] = nb[q];
+                }
+            }
+            if (i + 1 < steps) fetch(i + 1);
+            if (!mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
+            const uint32_t dst = ring0 + s * p.stage_bytes + ML_A_BYTES;
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                const int id = q * 128 + t;
+                if (id < chunks) {
+                    const uint32_t row = (uint32_t)id >> 3, at = row * 128u + (((uint32_t)id & 7u) ^ (row & 7u)) * 16u;
+#pragma unroll
+                    for (int e = 0; e < TERMS; ++e) sts128(dst + e * term_bytes + at, u[q][e]);
+                }
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(xfull0 + 8 * s);
+            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+        }
+    }
+
+    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, 2 * (kt1 - kt0), TERMS == 3);
+    drain_after_abort(abort_flag);
+    if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
+}
+
+// Tile, split and rings of one call; false when the sizes do not fit the grid.
+inline bool ml_plan(MlParams& p, bool f32_terms, bool by_threads, int sms) {
+    const int cap = f32_terms ? 64 : by_threads || p.o.y_f32 ? 128 : 256;
+    const int tiles = (p.o.M + cap - 1) / cap;
+    p.o.nt = ((p.o.M + tiles - 1) / tiles + 15) / 16 * 16;
+    const int wts = (int)(((long long)p.o.cols + 127) / 128);
+    const int tok_tiles = (p.o.M + p.o.nt - 1) / p.o.nt;
+    p.red_tiles = (int)(((long long)p.red + 127) / 128);
+    p.o.n_acc = f32_terms ? 5 : (512 / p.o.nt < 4 ? 512 / p.o.nt : 4);
+    p.tmem_cols = 32;
+    while (p.tmem_cols < (uint32_t)(p.o.n_acc * p.o.nt)) p.tmem_cols *= 2;
+    // as many CTAs as there are SMs, at least two pieces each; fp32 results: at most 128 additions into an accumulator
+    p.o.split = 1;
+    const long long ctas = (long long)wts * tok_tiles;
+    while (p.o.split < 8 && p.o.split * 4 <= p.red_tiles && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
+    if (p.o.y_f32) {
+        const int lead = f32_terms ? p.o.n_acc - 1 : p.o.n_acc;
+        while (p.o.split < 8 && p.o.split * 4 <= p.red_tiles && (long long)p.red_tiles * 8 > 128LL * lead * p.o.split) p.o.split *= 2;
+    }
+    p.stage_bytes = ML_A_BYTES + (uint32_t)p.o.nt * 128u * (f32_terms ? 3u : 1u);
+    p.code_stages = p.o.nt > 128 ? 3 : 6;
+    const size_t room = ML_SMEM_MOST - (size_t)p.code_stages * ((ML_CODE_BYTES + 127) / 128 * 128);
+    p.stages = (int)(room / p.stage_bytes);
+    if (p.stages > ML_MAX_STAGES) p.stages = ML_MAX_STAGES;
+    p.code_at = (uint32_t)p.stages * p.stage_bytes;
+    return (long long)wts * p.o.split <= 0x7fffffffLL && tok_tiles <= 65535;
+}
+
+}  // namespace pac

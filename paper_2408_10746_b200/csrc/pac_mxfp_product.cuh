@@ -1,0 +1,150 @@
+// Product of two matrices in MXFP4 (pac_mxfp.cuh): y = A B^T, A [M][K] tokens, B [N][K] a frozen matrix.
+//
+// tcgen05.mma kind::mxf4 multiplies packed codes and applies both operands' scales itself: K steps of 64 values, fp32
+// accumulators, four times the bf16 rate.  Codes and scales go from memory to shared memory as they are (TMA boxes of 128
+// bytes of a row = 256 values; bulk copies of the scales' pieces), tcgen05.cp spreads a piece over tensor memory (row r:
+// lane r % 32 of every quadrant, column r / 32, four scales to a 32-bit word), and no thread touches an operand.  As in
+// pac_mxfp_linear.cuh the frozen matrix is the M operand and the tokens are the N operand.
+#pragma once
+#include "pac_mxfp_linear.cuh"
+
+namespace pac {
+
+constexpr int MP_BK = 256, MP_MAX_STAGES = 8;
+constexpr uint32_t MP_W_BYTES = 128 * 128;
+constexpr uint32_t MP_SF_COL = 384;                          // scales in tensor memory: two sets of up to 24 columns from here on
+
+struct MpParams {
+    MxOut o;
+    const unsigned char *a_scales, *b_scales;
+    int pieces;                                             // pieces of scales per row tile (even)
+    int steps;                                              // ceil(K / 256)
+    int stages;
+    uint32_t x_bytes, stage_bytes;
+};
+
+// D[tmem] (+)= A B with one scale per 32 values of a row; sf: tensor-memory addresses of the scales.
+__device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// 32 rows of 16 bytes of shared memory -> 32 lanes x 4 columns, the same in all four quadrants.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// Shared-memory descriptor without a swizzle: groups of 8 rows of 16 bytes, 128 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_plain(uint32_t saddr) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+}
+// Instruction descriptor, kind::mxf4: A and B E2M1 (bits 7, 10), both K-major, N >> 3 at bit 17, scales UE8M0 (bit 23), M >> 7 at
+// bit 27; which half of a word of scales this K step uses (0 or 2): bits 4 (B) and 29 (A).
+__device__ __forceinline__ uint32_t instr_desc_mxf4(int N, uint32_t half) {
+    return (half << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | (1u << 27) | (half << 29);
+}
+
+// Warps: 0 copies, 1 scales and MMAs, 2-9 store y.
+__global__ void __launch_bounds__(320, 1) mxfp_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MpParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    __shared__ __align__(8) unsigned long long bars[2 * MP_MAX_STAGES + 1];
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ int abort_sh;
+    const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[MP_MAX_STAGES]), accf = smem_u32(&bars[2 * MP_MAX_STAGES]);
+    const int warp = threadIdx.x >> 5;
+    const int rank = p.o.split > 1 ? (int)(blockIdx.x % p.o.split) : 0;
+    const int wt = blockIdx.x / p.o.split, t0 = blockIdx.y * p.o.nt;
+    const int k0 = (int)((long long)p.steps * rank / p.o.split), k1 = (int)((long long)p.steps * (rank + 1) / p.o.split);
+    const uint32_t ring0 = smem_u32(smem);
+    // pieces of scales that the tile's tokens lie in (t0 is a multiple of 128); past the last row there are none
+    const int t_tiles = (int)min((long long)(p.o.nt + 127) / 128, ((long long)p.o.M - t0 + 127) / 128);
+
+    if (threadIdx.x == 0) {
+        abort_sh = 0;
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+        mbar_init(accf, 1);
+        fence_mbar_init();
+        tma_prefetch_desc(&map_a);
+        tma_prefetch_desc(&map_b);
+    }
+    if (warp == 1) { tmem_alloc(smem_u32(&tmem_base_sh), 512u); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_base_sh;
+    volatile int* abort_flag = &abort_sh;
+    // a stage: codes of the matrix, codes of the tokens, scales of the matrix (2 pieces), scales of the tokens (2 per 128)
+    const uint32_t sf_at = MP_W_BYTES + p.x_bytes;
+
+    if (warp == 0) {
+        uint32_t s = 0, ph = 1;
+        for (int k = k0; k < k1; ++k) {
+            if (!mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
+            if (elect_one()) {
+                const uint32_t bar = full0 + 8 * s, dst = ring0 + s * p.stage_bytes;
+                mbar_expect_tx(bar, MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (1 + t_tiles));
+                ml_tma_2d(dst, &map_b, bar, k * 128, wt * 128);
+                ml_tma_2d(dst + MP_W_BYTES, &map_a, bar, k * 128, t0);
+                bulk_load_1d(dst + sf_at, p.b_scales + ((long long)wt * p.pieces + 2 * k) * MX_SCALE_PIECE, 2 * MX_SCALE_PIECE, bar);
+                for (int i = 0; i < t_tiles; ++i)
+                    bulk_load_1d(dst + sf_at + 2 * MX_SCALE_PIECE * (1 + i), p.a_scales + ((long long)(t0 / 128 + i) * p.pieces + 2 * k) * MX_SCALE_PIECE,
+                                 2 * MX_SCALE_PIECE, bar);
+            }
+            __syncwarp();
+            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+        }
+    } else if (warp == 1) {
+        const uint32_t idesc0 = instr_desc_mxf4(p.o.nt, 0u), idesc1 = instr_desc_mxf4(p.o.nt, 2u);
+        const uint64_t w0 = smem_desc_sw128(ring0, 16, 1024), x0 = smem_desc_sw128(ring0 + MP_W_BYTES, 16, 1024), f0 = smem_desc_plain(ring0 + sf_at);
+        uint32_t s = 0, ph = 0, acc = 0;
+        for (int i = 0; i < k1 - k0; ++i) {
+            if (!mbar_wait_uniform(full0 + 8 * s, ph, abort_flag, nullptr)) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
+                const uint32_t sf = tmem_base + MP_SF_COL + (i & 1) * 32u;   // copies and MMAs of one thread take effect in order
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {                // 128 values of K: one word of scales per row
+                    tmem_copy_scales(sf + c * 4, f0 + off + c * (MX_SCALE_PIECE >> 4));
+                    for (int t = 0; t < t_tiles; ++t)
+                        tmem_copy_scales(sf + 8 + c * 8 + t * 4, f0 + off + (2 * (1 + t) + c) * (MX_SCALE_PIECE >> 4));
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    umma_mxf4(tmem_base + acc * p.o.nt, w0 + off + 2 * k, x0 + off + 2 * k, (k & 1) ? idesc1 : idesc0, sf + (k >> 1) * 4, sf + 8 + (k >> 1) * 8,
+                              (i >= p.o.n_acc || k) ? 1u : 0u);
+                umma_commit(empty0 + 8 * s);
+            }
+            __syncwarp();
+            if (++acc == (uint32_t)p.o.n_acc) acc = 0;
+            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+        }
+        if (elect_one()) umma_commit(accf);
+        __syncwarp();
+    }
+    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, k1 - k0, false);
+    drain_after_abort(abort_flag);
+    if (warp == 1) tmem_dealloc(tmem_base, 512u);
+}
+
+inline bool mp_plan(MpParams& p, int K, int sms) {
+    const int cap = p.o.y_f32 ? 128 : 256;
+    // several token tiles begin at multiples of 128, where the pieces of scales do
+    p.o.nt = p.o.M <= cap ? (p.o.M + 15) / 16 * 16 : cap;
+    const int tok_tiles = (p.o.M + p.o.nt - 1) / p.o.nt;
+    const long long wts = ((long long)p.o.cols + 127) / 128, ctas = wts * tok_tiles;
+    p.steps = (int)(((long long)K + MP_BK - 1) / MP_BK);
+    p.o.n_acc = 384 / p.o.nt < 3 ? 384 / p.o.nt : 3;
+    p.o.split = 1;
+    while (p.o.split < 8 && p.o.split * 2 <= p.steps && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
+    // fp32 results: at most 128 additions (of 64 products each) into an accumulator
+    while (p.o.y_f32 && p.o.split < 8 && p.o.split * 2 <= p.steps && (long long)p.steps * 4 > 128LL * p.o.n_acc * p.o.split) p.o.split *= 2;
+    p.x_bytes = (uint32_t)p.o.nt * 128u;
+    p.stage_bytes = MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (uint32_t)(1 + (p.o.nt + 127) / 128);
+    p.stage_bytes = (p.stage_bytes + 1023u) / 1024u * 1024u;
+    p.stages = (int)(ML_SMEM_MOST / p.stage_bytes);
+    if (p.stages > MP_MAX_STAGES) p.stages = MP_MAX_STAGES;
+    return wts * p.o.split <= 0x7fffffffLL && tok_tiles <= 65535;
+}
+
+}  // namespace pac

@@ -6,7 +6,7 @@
 // u_l = h_l W_down^l, z_l = lambda_l u_l + (1-lambda_l) a_{l-1}, a_l = phi(z_l),
 // y = h_L + a_L W_up.
 #pragma once
-#include "pac_common.cuh"
+#include "pac_adamw.cuh"
 
 namespace pac {
 
@@ -492,20 +492,6 @@ __global__ void mean_kernel(const float* __restrict__ x, int n, float* __restric
 // only).  bc1 = 1-beta1^t, bc2 = 1-beta2^t (bias corrections, computed on the host in double).  Also refreshes the bf16
 // terms of W_down that the tensor-core path multiplies with.
 // ---------------------------------------------------------------------------
-// One element of the update, shared by every kernel that applies AdamW so that fused and
-// separate updates are bit-identical.
-// The arithmetic of one element: returns the new parameter, updates mi / vi in place.
-__device__ __forceinline__ float adamw_math(float th, float& mi, float& vi, float gi, bool decays, const pac_adamw& hp,
-                                            float bc1, float bc2) {
-    // every rounding is spelled out (no contraction into FMAs), in the order the update is written:
-    // m = b1 m + (1-b1) g;  v = b2 v + ((1-b2) g) g;  theta = (theta - lr wd theta) - (lr mhat)/(sqrt(vhat)+eps)
-    mi = __fadd_rn(__fmul_rn(hp.beta1, mi), __fmul_rn(__fsub_rn(1.f, hp.beta1), gi));
-    vi = __fadd_rn(__fmul_rn(hp.beta2, vi), __fmul_rn(__fmul_rn(__fsub_rn(1.f, hp.beta2), gi), gi));
-    const float mhat = __fdiv_rn(mi, bc1), vhat = __fdiv_rn(vi, bc2);
-    const float decay = decays ? __fmul_rn(__fmul_rn(hp.lr, hp.weight_decay), th) : 0.f;
-    return __fsub_rn(__fsub_rn(th, decay), __fdiv_rn(__fmul_rn(hp.lr, mhat), __fadd_rn(__fsqrt_rn(vhat), hp.eps)));
-}
-
 __device__ __forceinline__ void adamw_element(float* __restrict__ p, float* __restrict__ m, float* __restrict__ v,
                                               long long i, float gi, const ParamLayout& lay, const pac_adamw& hp,
                                               float bc1, float bc2, WdShadow wdT, int d, int r) {
