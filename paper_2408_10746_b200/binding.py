@@ -489,33 +489,50 @@ def dequantize_absmax(q, c, block: int, device: int = 0, stream: Optional[int] =
 # MXFP4: frozen matrices and hidden states in 4 bits, and products with them.  Every call runs on the device of its
 # tensors and on torch's current stream there.
 # ---------------------------------------------------------------------------
-def _invalid(what: str, ok: bool):
-    if not ok:
-        raise PacError(1, what)
+def _refuse(what: str):
+    raise PacError(1, what)
+
+
+_DTYPES = {}
 
 
 def _dtype(t):
-    import torch
-    code = {torch.float32: PAC_F32, torch.bfloat16: PAC_BF16}.get(t)
-    _invalid(f"values are float32 or bfloat16, not {t}", code is not None)
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: PAC_F32, torch.bfloat16: PAC_BF16})
+    code = _DTYPES.get(t)
+    if code is None:
+        _refuse(f"values are float32 or bfloat16, not {t}")
     return code
 
 
-def _stream(device):
-    import torch
-    return torch.cuda.current_stream(device).cuda_stream
+_RAW_STREAM = None
+
+
+def _stream(index: int) -> int:
+    """Handle of torch's current stream on a device (torch's own quick way to it where it has one: 0.2 us instead of 1.5)."""
+    global _RAW_STREAM
+    if _RAW_STREAM is None:
+        import torch
+        _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _RAW_STREAM(index)
 
 
 def _rows(t, name: str):
     """A CUDA matrix with consecutive elements along its rows: (rows, columns, elements from row to row)."""
-    _invalid(f"{name} is a 2-D CUDA tensor", t.is_cuda and t.dim() == 2)
+    if not t.is_cuda or t.dim() != 2:
+        _refuse(f"{name} is a 2-D CUDA tensor")
     rows, cols = t.shape
-    _invalid(f"{name} has at least one column", cols > 0)
+    if cols < 1:
+        _refuse(f"{name} has at least one column")
+    step, ld = t.stride(1), t.stride(0)
+    if cols > 1 and step != 1 and rows:
+        _refuse(f"{name}: elements of a row are consecutive")
     if rows <= 1:
-        _invalid(f"{name}: elements of a row are consecutive", cols == 1 or t.stride(1) == 1 or t.numel() == 0)
         return rows, cols, cols
-    _invalid(f"{name}: elements of a row are consecutive, rows do not overlap", (cols == 1 or t.stride(1) == 1) and t.stride(0) >= cols)
-    return rows, cols, t.stride(0)
+    if ld < cols:
+        _refuse(f"{name}: rows do not overlap")
+    return rows, cols, ld
 
 
 def mxfp_shapes(rows: int, cols: int):
@@ -526,13 +543,15 @@ def mxfp_shapes(rows: int, cols: int):
 def _mxfp(codes, scales, cols: int, device=None):
     """Rows of an MXFP4 matrix of `cols` columns, its layout checked."""
     import torch
-    _invalid("codes and scales are contiguous CUDA uint8 tensors", codes.is_cuda and scales.is_cuda and codes.dtype == scales.dtype == torch.uint8
-             and codes.dim() == 2 and codes.is_contiguous() and scales.is_contiguous() and cols > 0)
+    if not (codes.is_cuda and scales.is_cuda and codes.dtype is torch.uint8 and scales.dtype is torch.uint8 and codes.dim() == 2
+            and codes.is_contiguous() and scales.is_contiguous() and cols > 0):
+        _refuse("codes and scales are contiguous CUDA uint8 tensors")
     rows = codes.shape[0]
     want = mxfp_shapes(rows, cols)
-    _invalid(f"{rows} x {cols} values have codes and scales of shapes {want}, not {tuple(codes.shape)} and {tuple(scales.shape)}",
-             tuple(codes.shape) == want[0] and tuple(scales.shape) == want[1])
-    _invalid("all tensors are on one device", codes.device == scales.device and (device is None or codes.device == device))
+    if codes.shape != want[0] or scales.shape != want[1]:
+        _refuse(f"{rows} x {cols} values have codes and scales of shapes {want}, not {tuple(codes.shape)} and {tuple(scales.shape)}")
+    if codes.device != scales.device or (device is not None and codes.device != device):
+        _refuse("all tensors are on one device")
     return rows
 
 
@@ -541,7 +560,8 @@ def _out(out, rows: int, cols: int, dtype, device):
     import torch
     if out is None:
         return torch.empty((rows, cols), dtype=dtype, device=device), cols
-    _invalid(f"out is {rows} x {cols} {dtype} on {device}", tuple(out.shape) == (rows, cols) and out.dtype == dtype and out.device == device)
+    if out.shape != (rows, cols) or out.dtype != dtype or out.device != device:
+        _refuse(f"out is {rows} x {cols} {dtype} on {device}")
     return out, _rows(out, "out")[2]
 
 
@@ -550,13 +570,15 @@ def quantize_mxfp(x, codes=None, scales=None):
     of two per 32 columns.  Shapes as mxfp_shapes gives; codes and scales may be given to be written into."""
     import torch
     rows, cols, ld = _rows(x, "x")
-    shapes = mxfp_shapes(rows, cols)
-    if codes is None:
-        codes = torch.empty(shapes[0], dtype=torch.uint8, device=x.device)
-    if scales is None:
-        scales = torch.empty(shapes[1], dtype=torch.uint8, device=x.device)
-    _invalid(f"codes have {shapes[0][0]} rows", _mxfp(codes, scales, cols, x.device) == rows)
-    st = load_library().pac_quantize_mxfp(x.device.index, _stream(x.device), x.data_ptr(), _dtype(x.dtype), rows, cols, ld, codes.data_ptr(), scales.data_ptr())
+    device, dtype = x.device, _dtype(x.dtype)
+    if codes is None or scales is None:
+        shapes = mxfp_shapes(rows, cols)
+        codes = torch.empty(shapes[0], dtype=torch.uint8, device=device) if codes is None else codes
+        scales = torch.empty(shapes[1], dtype=torch.uint8, device=device) if scales is None else scales
+    if _mxfp(codes, scales, cols, device) != rows:
+        _refuse(f"codes have {rows} rows")
+    index = device.index
+    st = load_library().pac_quantize_mxfp(index, _stream(index), x.data_ptr(), dtype, rows, cols, ld, codes.data_ptr(), scales.data_ptr())
     if st != 0:
         raise PacError(st, "pac_quantize_mxfp failed")
     return codes, scales
@@ -566,51 +588,54 @@ def dequantize_mxfp(codes, scales, cols: int, dtype=None, out=None):
     """The matrix [rows][cols] that codes and scales stand for, bfloat16 (exact) or float32."""
     import torch
     rows = _mxfp(codes, scales, cols)
+    device = codes.device
     dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
     code = _dtype(dtype)
-    out, ld = _out(out, rows, cols, dtype, codes.device)
-    st = load_library().pac_dequantize_mxfp(codes.device.index, _stream(codes.device), codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), code, ld)
+    out, ld = _out(out, rows, cols, dtype, device)
+    st = load_library().pac_dequantize_mxfp(device.index, _stream(device.index), codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), code, ld)
     if st != 0:
         raise PacError(st, "pac_dequantize_mxfp failed")
     return out
 
 
-def _mxfp_linear(name: str, x, codes, scales, N: int, K: int, cols: int, dtype, out):
-    M, _, ld = _rows(x, "x")
+def _mxfp_linear(call, x, M: int, ld: int, codes, scales, N: int, K: int, cols: int, dtype, out):
     dtype = dtype or (out.dtype if out is not None else x.dtype)
-    xt, yt = _dtype(x.dtype), _dtype(dtype)
-    out, ldo = _out(out, M, cols, dtype, x.device)
-    st = getattr(load_library(), name)(x.device.index, _stream(x.device), x.data_ptr(), xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K,
-                                       out.data_ptr(), yt, ldo)
+    device, xt, yt = x.device, _dtype(x.dtype), _dtype(dtype)
+    out, ldo = _out(out, M, cols, dtype, device)
+    st = call(device.index, _stream(device.index), x.data_ptr(), xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K, out.data_ptr(), yt, ldo)
     if st != 0:
-        raise PacError(st, f"{name} failed")
+        raise PacError(st, f"{call.__name__} failed")
     return out
 
 
 def mxfp_linear(x, codes, scales, dtype=None, out=None):
     """y = x W^T [M][N] for x [M][K] and a frozen W [N][K] in MXFP4 (quantize_mxfp); x and y float32 or bfloat16."""
-    K = _rows(x, "x")[1]
+    M, K, ld = _rows(x, "x")
     N = _mxfp(codes, scales, K, x.device)
-    _invalid("W has at least one row", N > 0)
-    return _mxfp_linear("pac_mxfp_linear", x, codes, scales, N, K, N, dtype, out)
+    if N < 1:
+        _refuse("W has at least one row")
+    return _mxfp_linear(load_library().pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out)
 
 
 def mxfp_linear_grad(dy, codes, scales, cols: int, dtype=None, out=None):
     """The backward pass of mxfp_linear: dx = dy W [M][cols] for dy [M][N]; W is frozen and has no gradient."""
-    N = _mxfp(codes, scales, cols, dy.device)
-    _invalid(f"dy has {N} columns, one per row of W", _rows(dy, "dy")[1] == N)
-    return _mxfp_linear("pac_mxfp_linear_grad", dy, codes, scales, N, cols, cols, dtype, out)
+    M, N, ld = _rows(dy, "dy")
+    if _mxfp(codes, scales, cols, dy.device) != N:
+        _refuse(f"dy has {N} columns, one per row of W")
+    return _mxfp_linear(load_library().pac_mxfp_linear_grad, dy, M, ld, codes, scales, N, cols, cols, dtype, out)
 
 
 def mxfp_product(a_codes, a_scales, b_codes, b_scales, cols: int, dtype=None, out=None):
     """A B^T [M][N] of two MXFP4 matrices of `cols` columns each, bfloat16 or float32."""
     import torch
-    M, N = _mxfp(a_codes, a_scales, cols), _mxfp(b_codes, b_scales, cols, a_codes.device)
-    _invalid("B has at least one row", N > 0)
+    device = a_codes.device
+    M, N = _mxfp(a_codes, a_scales, cols), _mxfp(b_codes, b_scales, cols, device)
+    if N < 1:
+        _refuse("B has at least one row")
     dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
     code = _dtype(dtype)
-    out, ldo = _out(out, M, N, dtype, a_codes.device)
-    st = load_library().pac_mxfp_product(a_codes.device.index, _stream(a_codes.device), a_codes.data_ptr(), a_scales.data_ptr(), M, b_codes.data_ptr(),
+    out, ldo = _out(out, M, N, dtype, device)
+    st = load_library().pac_mxfp_product(device.index, _stream(device.index), a_codes.data_ptr(), a_scales.data_ptr(), M, b_codes.data_ptr(),
                                          b_scales.data_ptr(), N, cols, out.data_ptr(), code, ldo)
     if st != 0:
         raise PacError(st, "pac_mxfp_product failed")
@@ -620,6 +645,11 @@ def mxfp_product(a_codes, a_scales, b_codes, b_scales, cols: int, dtype=None, ou
 # ---------------------------------------------------------------------------
 # AdamW over a list of tensors
 # ---------------------------------------------------------------------------
+def _want(what: str, ok: bool):
+    if not ok:
+        _refuse(what)
+
+
 class AdamWTensors:
     """AdamW over a list of CUDA tensors (float32 or bfloat16, contiguous, all on one device) with moments in float32 (bits=32) or
     in 8 bits (bits=8: float8_e4m3fn codes, the second moment as its root, one float32 constant per 256 elements).
@@ -632,10 +662,10 @@ class AdamWTensors:
     def __init__(self, params, grads, bits: int = 32, state=None, decay=None, steps: int = 0, seed: int = 0):
         import torch
         params, grads = list(params), list(grads)
-        _invalid("bits is 8 or 32", bits in (8, 32))
-        _invalid("one gradient per parameter", len(params) == len(grads))
+        _want("bits is 8 or 32", bits in (8, 32))
+        _want("one gradient per parameter", len(params) == len(grads))
         decay = [True] * len(params) if decay is None else list(decay)
-        _invalid("one truth value of decay per parameter", len(decay) == len(params))
+        _want("one truth value of decay per parameter", len(decay) == len(params))
         blocks = [(p.numel() + 255) // 256 for p in params]
         if state is None:
             held = torch.float32 if bits == 32 else torch.float8_e4m3fn
@@ -644,25 +674,25 @@ class AdamWTensors:
             if bits == 8:
                 state.update({k: [zeros(b, p, torch.float32) for p, b in zip(params, blocks)] for k in ("m_scale", "v_scale")})
         names = ("m", "v", "m_scale", "v_scale") if bits == 8 else ("m", "v")
-        _invalid(f"state has the lists {names}", sorted(state) == sorted(names) and all(len(state[k]) == len(params) for k in names))
+        _want(f"state has the lists {names}", sorted(state) == sorted(names) and all(len(state[k]) == len(params) for k in names))
         self.device = params[0].device if params else None
         spans = []
         for i, (p, g, b) in enumerate(zip(params, grads, blocks)):
-            _invalid(f"tensor {i}: gradient of the parameter's shape", p.shape == g.shape)
+            _want(f"tensor {i}: gradient of the parameter's shape", p.shape == g.shape)
             parts = [(p, None, p.numel()), (g, None, p.numel())]
             held = torch.float32 if bits == 32 else torch.float8_e4m3fn
             parts += [(state[k][i], held, p.numel()) for k in ("m", "v")]
             parts += [(state[k][i], torch.float32, b) for k in names[2:]]
             for j, (t, want, n) in enumerate(parts):
-                _invalid(f"tensor {i}: contiguous tensors on {self.device}", t.is_cuda and t.device == self.device and t.is_contiguous())
-                _invalid(f"tensor {i}: {n} elements of moments, {b} constants, of their types", t.numel() == n and want in (None, t.dtype))
+                _want(f"tensor {i}: contiguous tensors on {self.device}", t.is_cuda and t.device == self.device and t.is_contiguous())
+                _want(f"tensor {i}: {n} elements of moments, {b} constants, of their types", t.numel() == n and want in (None, t.dtype))
                 if n:
                     spans.append((t.data_ptr(), t.data_ptr() + n * t.element_size(), j != 1))
         # what is written may overlap nothing else
         spans.sort()
         end, end_w = 0, 0
         for a, b, w in spans:
-            _invalid("no two of the tensors overlap", a >= (end if w else end_w))
+            _want("no two of the tensors overlap", a >= (end if w else end_w))
             end, end_w = max(end, b), max(end_w, b if w else 0)
         self._keep = (params, grads, state)
         self.bits, self.steps, self.seed, self._state = bits, int(steps), int(seed) & 0xFFFFFFFF, state
@@ -678,16 +708,16 @@ class AdamWTensors:
     def step(self, hp: AdamW, grad_scale: float = 1.0, step=None):
         """One update.  step: None counts on from `steps`; a CUDA int64 tensor of one element holds the number of the step on the
         device (from 1; the caller moves it on), which a step captured into a graph needs."""
-        import torch
         if self._count == 0:
             return
         dev = None
         if step is not None:
-            _invalid("step is a CUDA int64 tensor of one element", torch.is_tensor(step) and step.device == self.device and step.dtype == torch.int64
-                     and step.numel() == 1)
+            import torch
+            _want("step is a CUDA int64 tensor of one element", torch.is_tensor(step) and step.device == self.device and step.dtype == torch.int64
+                  and step.numel() == 1)
             dev = step.data_ptr()
-        st = load_library().pac_adamw_tensors(self.device.index, _stream(self.device), self._list, self._count, self.bits, C.byref(hp._c()), self.steps + 1, dev,
-                                              grad_scale, self.seed)
+        index = self.device.index
+        st = load_library().pac_adamw_tensors(index, _stream(index), self._list, self._count, self.bits, hp._c(), self.steps + 1, dev, grad_scale, self.seed)
         if st != 0:
             raise PacError(st, "pac_adamw_tensors failed" + (": under capture the step's number has to be on the device" if st == 2 else ""))
         if dev is None:

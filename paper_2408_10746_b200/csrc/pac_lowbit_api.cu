@@ -1,6 +1,7 @@
 // C entries of what a trainer keeps in few bits: the MXFP4 codec and its products, and the AdamW step over a list of
 // tensors.  None of them allocates device memory or keeps anything from call to call; all work is enqueued on the
 // caller's stream and may be captured.
+#include <atomic>
 #include <cmath>
 
 #include "pac_adamw_tensors.cuh"
@@ -31,9 +32,15 @@ bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; 
 bool dtype_ok(int t) { return t == PAC_F32 || t == PAC_BF16; }
 size_t dtype_size(int t) { return t == PAC_F32 ? 4 : 2; }
 
+constexpr int MOST_DEVICES = 64;
 int sm_count(int device) {
-    int n = 0;
-    return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) == cudaSuccess && n > 0 ? n : 148;
+    static std::atomic<int> known[MOST_DEVICES];
+    const bool keep = device >= 0 && device < MOST_DEVICES;
+    int n = keep ? known[device].load(std::memory_order_relaxed) : 0;
+    if (n > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) { cudaGetLastError(); return 148; }
+    if (keep) known[device].store(n, std::memory_order_relaxed);
+    return n;
 }
 pac_status launched() { return cudaGetLastError() == cudaSuccess ? PAC_OK : PAC_ERR_CUDA; }
 
@@ -53,13 +60,22 @@ bool matrix_ok(const void* codes, const void* scales, long long rows, int cols) 
     return codes && scales && aligned(codes, 16) && aligned(scales, 16) && rows >= 1 && rows <= 0x7fffff00LL && cols >= 1 && cols <= 0x7fffff00;
 }
 
-cudaError_t opt_in(const void* kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
+// Opts a kernel in to all the dynamic shared memory it may ever ask for, once per device; `done` is the kernel's own.
+struct OptedIn { std::atomic<bool> on[MOST_DEVICES]; };
+cudaError_t opt_in(OptedIn& done, const void* kernel, int device) {
+    const bool keep = device >= 0 && device < MOST_DEVICES;
+    if (keep && done.on[device].load(std::memory_order_acquire)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(ML_SMEM_MOST + 1024));
+    if (e == cudaSuccess && keep) done.on[device].store(true, std::memory_order_release);
+    return e;
+}
 
 template <bool GRAD, int XMODE>
-cudaError_t launch_linear(cudaStream_t st, const CUtensorMap& codes, const CUtensorMap& x, const MlParams& p) {
+cudaError_t launch_linear(int device, cudaStream_t st, const CUtensorMap& codes, const CUtensorMap& x, const MlParams& p) {
     const auto kernel = mxfp_linear_kernel<GRAD, XMODE>;
     const size_t smem = 1024 + p.code_at + (size_t)p.code_stages * ML_CODE_BYTES;
-    cudaError_t e = opt_in((const void*)kernel, smem);
+    static OptedIn done;
+    cudaError_t e = opt_in(done, (const void*)kernel, device);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(((p.o.cols + 127LL) / 128) * p.o.split), (unsigned)((p.o.M + p.o.nt - 1) / p.o.nt));
@@ -97,11 +113,11 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
     if (grad)
-        e = mode == ML_X_TMA ? launch_linear<true, ML_X_TMA>(st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<true, ML_X_BF16>(st, mc, mx, p)
-                                                                                                 : launch_linear<true, ML_X_F32>(st, mc, mx, p);
+        e = mode == ML_X_TMA ? launch_linear<true, ML_X_TMA>(device, st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<true, ML_X_BF16>(device, st, mc, mx, p)
+                                                                                                 : launch_linear<true, ML_X_F32>(device, st, mc, mx, p);
     else
-        e = mode == ML_X_TMA ? launch_linear<false, ML_X_TMA>(st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<false, ML_X_BF16>(st, mc, mx, p)
-                                                                                                  : launch_linear<false, ML_X_F32>(st, mc, mx, p);
+        e = mode == ML_X_TMA ? launch_linear<false, ML_X_TMA>(device, st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<false, ML_X_BF16>(device, st, mc, mx, p)
+                                                                                                  : launch_linear<false, ML_X_F32>(device, st, mc, mx, p);
     if (e != cudaSuccess) { cudaGetLastError(); return PAC_ERR_CUDA; }
     return PAC_OK;
 }
@@ -170,7 +186,8 @@ extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsi
         !map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, dev_b_codes, mx_row_bytes(K), N, mx_row_bytes(K), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))
         return PAC_ERR_CUDA;
     const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes;
-    cudaError_t e = opt_in((const void*)mxfp_product_kernel, smem);
+    static OptedIn done;
+    cudaError_t e = opt_in(done, (const void*)mxfp_product_kernel, device);
     if (e == cudaSuccess) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(((N + 127LL) / 128) * p.o.split), (unsigned)((M + p.o.nt - 1) / p.o.nt));
@@ -193,22 +210,29 @@ extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsi
 // ---------------------------------------------------------------------------
 namespace {
 
+unsigned long long blocks_of(const pac_adamw_tensor& t) { return (unsigned long long)((t.n + AT_BLOCK - 1) / AT_BLOCK); }
+
 template <int BITS, int CAP>
 cudaError_t launch_adamw(cudaStream_t st, const pac_adamw_tensor* t, int count, AtStep s, int sms) {
     AtList<CAP> list;
-    unsigned long long blocks = 0;
+    unsigned long long blocks = 0, chunks = 0;
+    for (int i = 0; i < count; ++i) blocks += blocks_of(t[i]);
+    // a chunk is what one warp takes at a time (its next block is on the way while one is computed): one wave of warps where 16
+    // blocks or fewer to each are enough (8.65 M fp32 elements: 33 us at four blocks, in 2.4 waves)
+    const unsigned long long resident = (unsigned long long)sms * 24, per = (blocks + resident - 1) / resident;
+    s.chunk = per < 1 ? 1u : per > 16 ? 16u : (uint32_t)per;
     for (int i = 0; i < count; ++i) {
         AtTensor& a = list.t[i];
         a.p = t[i].p; a.g = t[i].g; a.m = t[i].m; a.v = t[i].v; a.m_scale = t[i].m_scale; a.v_scale = t[i].v_scale; a.n = t[i].n;
-        a.first_block = (uint32_t)blocks;
+        a.first_chunk = (uint32_t)chunks;
         const size_t pa = t[i].p_dtype == PAC_F32 ? 32 : 16, ga = t[i].g_dtype == PAC_F32 ? 32 : 16, sa = BITS == 32 ? 32 : 8;
         const bool vec = aligned(a.p, pa) && aligned(a.g, ga) && aligned(a.m, sa) && aligned(a.v, sa);
         a.flags = (t[i].p_dtype == PAC_BF16 ? AT_P16 : 0u) | (t[i].g_dtype == PAC_BF16 ? AT_G16 : 0u) | (t[i].decay ? AT_DECAY : 0u) | (vec ? AT_VEC : 0u);
-        blocks += (unsigned long long)((t[i].n + AT_BLOCK - 1) / AT_BLOCK);
+        chunks += (blocks_of(t[i]) + s.chunk - 1) / s.chunk;
     }
     s.count = count;
-    s.blocks = (uint32_t)blocks;
-    const unsigned long long want = (blocks + 7) / 8, most = (unsigned long long)sms * 32;
+    s.chunks = (uint32_t)chunks;
+    const unsigned long long want = (chunks + 7) / 8, most = (unsigned long long)sms * 32;
     adamw_tensors_kernel<BITS, CAP><<<(unsigned)(want < most ? want : most), 256, 0, st>>>(list, s);
     return cudaGetLastError();
 }
@@ -250,7 +274,7 @@ extern "C" pac_status pac_adamw_tensors(int device, void* cuda_stream, const pac
         while (at < count && tensors[at].n == 0) ++at;
         const int most = count - at <= AT_SMALL ? AT_SMALL : AT_LARGE;
         while (at + n < count && n < most && tensors[at + n].n > 0) {
-            const unsigned long long b = (unsigned long long)((tensors[at + n].n + AT_BLOCK - 1) / AT_BLOCK);
+            const unsigned long long b = blocks_of(tensors[at + n]);
             if (blocks + b > 0x7fffffffULL && n > 0) break;
             blocks += b;
             ++n;
