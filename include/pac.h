@@ -355,7 +355,12 @@ pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const unsigned cha
  * bounded; one that ran out, after about a second, leaves NaN in its part of y.) */
 pac_status pac_mxfp_linear(int device, void* cuda_stream, const void* dev_x, int x_dtype, int M, long long ldx,
                            const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_y, int y_dtype,
-                           long long ldy);
+                           long long ldy, void* dev_workspace, long long workspace_bytes);
+/* Bytes of the workspace (256-byte aligned) with which a call of up to 16 tokens takes its fast way: x as a sum of twelve
+ * matrices in MXFP4, then one block-scaled product.  There x enters to 2^-24 of the largest of its 32 neighbours in a block
+ * (bf16 values within 2^16 of each other: exactly).  0 for more tokens, which need none; without one (NULL) such a call takes
+ * the way of the larger ones.  The workspace belongs to the call until its work is done. */
+long long pac_mxfp_linear_workspace(int M, int K);
 /* Its backward pass: dx = dy W, dev_dy [M][N], dev_dx [M][K].  W is frozen and has no gradient. */
 pac_status pac_mxfp_linear_grad(int device, void* cuda_stream, const void* dev_dy, int dy_dtype, int M, long long lddy,
                                 const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_dx,

@@ -29,7 +29,7 @@ EXPORTS = ["pac_create", "pac_destroy", "pac_cache_register", "pac_cache_registe
            "pac_param_count", "pac_get_params", "pac_set_params", "pac_get_grads", "pac_get_opt_state",
            "pac_set_opt_state", "pac_set_option", "pac_device_buffers", "pac_params_changed", "pac_kernel_times", "pac_stream_phase_times", "pac_launch_count", "pac_sync", "pac_selftest_wait_expiry", "pac_selftest_rows_plan", "pac_selftest_second_pass_plan", "pac_last_error",
            "pac_kernel_path", "pac_eval_logits_static", "pac_quantize_absmax", "pac_dequantize_absmax",
-           "pac_quantize_mxfp", "pac_dequantize_mxfp", "pac_mxfp_linear", "pac_mxfp_linear_grad", "pac_mxfp_product", "pac_adamw_tensors"]
+           "pac_quantize_mxfp", "pac_dequantize_mxfp", "pac_mxfp_linear", "pac_mxfp_linear_workspace", "pac_mxfp_linear_grad", "pac_mxfp_product", "pac_adamw_tensors"]
 
 
 class PacError(RuntimeError):
@@ -122,12 +122,14 @@ def load_library() -> C.CDLL:
     lib.pac_dequantize_absmax.restype = I
     lib.pac_quantize_mxfp.argtypes = [I, P, P, I, LL, I, LL, P, P]
     lib.pac_dequantize_mxfp.argtypes = [I, P, P, P, LL, I, P, I, LL]
-    lib.pac_mxfp_linear.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL]
+    lib.pac_mxfp_linear.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL, P, LL]
     lib.pac_mxfp_linear_grad.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL]
     lib.pac_mxfp_product.argtypes = [I, P, P, P, I, P, P, I, I, P, I, LL]
     lib.pac_adamw_tensors.argtypes = [I, P, C.POINTER(_AdamWTensor), I, I, C.POINTER(_AdamW), LL, P, F, C.c_uint]
     for name in ("pac_quantize_mxfp", "pac_dequantize_mxfp", "pac_mxfp_linear", "pac_mxfp_linear_grad", "pac_mxfp_product", "pac_adamw_tensors"):
         getattr(lib, name).restype = I
+    lib.pac_mxfp_linear_workspace.argtypes = [I, I]
+    lib.pac_mxfp_linear_workspace.restype = LL
     lib.pac_last_error.argtypes = [P]
     lib.pac_last_error.restype = C.c_char_p
     lib.pac_kernel_path.argtypes = [P]
@@ -535,6 +537,9 @@ def _rows(t, name: str):
     return rows, cols, ld
 
 
+MXFP_FEW_TOKENS = 16          # calls of so many tokens go by way of a workspace
+
+
 def mxfp_shapes(rows: int, cols: int):
     """Shapes of the codes and of the scales (both uint8) of a rows x cols matrix."""
     return (rows, 16 * ((cols + 31) // 32)), ((rows + 127) // 128, 2 * ((cols + 255) // 256), 32, 4, 4)
@@ -598,11 +603,11 @@ def dequantize_mxfp(codes, scales, cols: int, dtype=None, out=None):
     return out
 
 
-def _mxfp_linear(call, x, M: int, ld: int, codes, scales, N: int, K: int, cols: int, dtype, out):
+def _mxfp_linear(call, x, M: int, ld: int, codes, scales, N: int, K: int, cols: int, dtype, out, *space):
     dtype = dtype or (out.dtype if out is not None else x.dtype)
     device, xt, yt = x.device, _dtype(x.dtype), _dtype(dtype)
     out, ldo = _out(out, M, cols, dtype, device)
-    st = call(device.index, _stream(device.index), x.data_ptr(), xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K, out.data_ptr(), yt, ldo)
+    st = call(device.index, _stream(device.index), x.data_ptr(), xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K, out.data_ptr(), yt, ldo, *space)
     if st != 0:
         raise PacError(st, f"{call.__name__} failed")
     return out
@@ -614,7 +619,13 @@ def mxfp_linear(x, codes, scales, dtype=None, out=None):
     N = _mxfp(codes, scales, K, x.device)
     if N < 1:
         _refuse("W has at least one row")
-    return _mxfp_linear(load_library().pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out)
+    lib = load_library()
+    if M > MXFP_FEW_TOKENS or M < 1:
+        return _mxfp_linear(lib.pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out, None, 0)
+    import torch
+    n = lib.pac_mxfp_linear_workspace(M, K)
+    space = torch.empty(n, dtype=torch.uint8, device=x.device)
+    return _mxfp_linear(lib.pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out, space.data_ptr(), n)
 
 
 def mxfp_linear_grad(dy, codes, scales, cols: int, dtype=None, out=None):

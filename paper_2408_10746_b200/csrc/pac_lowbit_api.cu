@@ -90,8 +90,57 @@ cudaError_t launch_linear(int device, cudaStream_t st, const CUtensorMap& codes,
     return cudaLaunchKernelEx(&cfg, kernel, codes, x, p);
 }
 
+// y = A B^T on the block-scaled tensor cores; `rows` of A's codes.
+cudaError_t launch_product(int device, cudaStream_t st, const unsigned char* a_codes, int rows, const unsigned char* b_codes, int K, MpParams& p) {
+    CUtensorMap ma, mb;
+    if (!map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, a_codes, mx_row_bytes(K), rows, mx_row_bytes(K), 128, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, b_codes, mx_row_bytes(K), p.o.cols, mx_row_bytes(K), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorInvalidValue;
+    static OptedIn done;
+    const cudaError_t e = opt_in(done, (const void*)mxfp_product_kernel, device);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(((p.o.cols + 127LL) / 128) * p.o.split), (unsigned)((rows + p.o.nt - 1) / p.o.nt));
+    cfg.blockDim = dim3(320);
+    cfg.dynamicSmemBytes = mp_smem(p);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    unsigned n = 0;
+    if (p.o.split > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)p.o.split; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (p.after) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, mxfp_product_kernel, ma, mb, p);
+}
+
+// A few tokens as sums of matrices in MXFP4 (split_mxfp_kernel), then one block-scaled product.
+cudaError_t few_tokens(int device, cudaStream_t st, const void* x, int x_dtype, int M, long long ldx, const unsigned char* codes, const unsigned char* scales,
+                       int N, int K, void* y, int y_dtype, long long ldy, unsigned char* space) {
+    const MsSpace w = ms_space(M, K);
+    MpParams p = {};
+    p.a_scales = space + w.scales; p.b_scales = scales; p.b_codes = codes;
+    p.x = x; p.ldx = ldx; p.x_f32 = x_dtype == PAC_F32; p.K = K;
+    p.after = true;
+    p.o.y = y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32; p.o.M = M; p.o.cols = N; p.o.terms = MS_TERMS;
+    p.pieces = mx_col_pieces(K);
+    if (!mp_plan(p, K, sm_count(device))) return cudaErrorInvalidValue;
+    const unsigned grid = (unsigned)(((long long)M * p.pieces * 4 + 7) / 8);
+    if (x_dtype == PAC_F32) split_mxfp_kernel<float><<<grid, 256, 0, st>>>((const float*)x, M, K, ldx, space + w.codes, space + w.scales);
+    else split_mxfp_kernel<bf16><<<grid, 256, 0, st>>>((const bf16*)x, M, K, ldx, space + w.codes, space + w.scales);
+    const cudaError_t e = cudaGetLastError();
+    return e != cudaSuccess ? e : launch_product(device, st, space + w.codes, M * MS_TERMS, codes, K, p);
+}
+
 pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x_dtype, int M, long long ldx, const unsigned char* codes,
-                       const unsigned char* scales, int N, int K, void* y, int y_dtype, long long ldy) {
+                       const unsigned char* scales, int N, int K, void* y, int y_dtype, long long ldy, void* space = nullptr, long long space_bytes = 0) {
     const int red = grad ? N : K, out_cols = grad ? K : N;
     if (M < 0 || !matrix_ok(codes, scales, N, K) || !dtype_ok(x_dtype) || !dtype_ok(y_dtype)) return PAC_ERR_INVALID_ARG;
     if (M == 0) return PAC_OK;
@@ -99,7 +148,15 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     if (!aligned(x, dtype_size(x_dtype)) || !aligned(y, dtype_size(y_dtype))) return PAC_ERR_INVALID_ARG;
     OnDevice on(device);
     if (!on.ok) return PAC_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (!grad && space && M <= MS_MOST_TOKENS) {
+        if (!aligned(space, 256) || space_bytes < ms_space(M, K).bytes) return PAC_ERR_INVALID_ARG;
+        if (few_tokens(device, st, x, x_dtype, M, ldx, codes, scales, N, K, y, y_dtype, ldy, (unsigned char*)space) == cudaSuccess) return PAC_OK;
+        cudaGetLastError();
+        return PAC_ERR_CUDA;
+    }
     MlParams p = {};
+    p.o.terms = 1;
     p.x = x; p.ldx = ldx; p.scales = scales; p.o.y = y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32;
     p.o.M = M; p.o.cols = out_cols; p.red = red; p.pieces = mx_col_pieces(K);
     const bool rows16 = aligned(x, 16) && (ldx * (long long)dtype_size(x_dtype)) % 16 == 0;
@@ -110,7 +167,6 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     if (!map_2d(&mc, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, mx_row_bytes(K), N, mx_row_bytes(K), 64, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) return PAC_ERR_CUDA;
     mx = mc;
     if (mode == ML_X_TMA && !map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, red, M, ldx * 2, ML_BK, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B)) return PAC_ERR_CUDA;
-    cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
     if (grad)
         e = mode == ML_X_TMA ? launch_linear<true, ML_X_TMA>(device, st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<true, ML_X_BF16>(device, st, mc, mx, p)
@@ -158,9 +214,12 @@ extern "C" pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const u
 }
 
 extern "C" pac_status pac_mxfp_linear(int device, void* cuda_stream, const void* dev_x, int x_dtype, int M, long long ldx, const unsigned char* dev_codes,
-                                      const unsigned char* dev_scales, int N, int K, void* dev_y, int y_dtype, long long ldy) {
-    return mxfp_linear(false, device, cuda_stream, dev_x, x_dtype, M, ldx, dev_codes, dev_scales, N, K, dev_y, y_dtype, ldy);
+                                      const unsigned char* dev_scales, int N, int K, void* dev_y, int y_dtype, long long ldy, void* dev_workspace,
+                                      long long workspace_bytes) {
+    return mxfp_linear(false, device, cuda_stream, dev_x, x_dtype, M, ldx, dev_codes, dev_scales, N, K, dev_y, y_dtype, ldy, dev_workspace, workspace_bytes);
 }
+
+extern "C" long long pac_mxfp_linear_workspace(int M, int K) { return M < 1 || M > MS_MOST_TOKENS || K < 1 || K > 0x7fffff00 ? 0 : ms_space(M, K).bytes; }
 
 extern "C" pac_status pac_mxfp_linear_grad(int device, void* cuda_stream, const void* dev_dy, int dy_dtype, int M, long long lddy,
                                            const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_dx, int dx_dtype,
@@ -180,29 +239,11 @@ extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsi
     p.a_scales = dev_a_scales; p.b_scales = dev_b_scales;
     p.o.y = dev_y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32; p.o.M = M; p.o.cols = N;
     p.pieces = mx_col_pieces(K);
+    p.o.terms = 1;
     if (!mp_plan(p, K, sm_count(device))) return PAC_ERR_UNSUPPORTED;
-    CUtensorMap ma, mb;
-    if (!map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, dev_a_codes, mx_row_bytes(K), M, mx_row_bytes(K), 128, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, dev_b_codes, mx_row_bytes(K), N, mx_row_bytes(K), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))
-        return PAC_ERR_CUDA;
-    const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes;
-    static OptedIn done;
-    cudaError_t e = opt_in(done, (const void*)mxfp_product_kernel, device);
-    if (e == cudaSuccess) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(((N + 127LL) / 128) * p.o.split), (unsigned)((M + p.o.nt - 1) / p.o.nt));
-        cfg.blockDim = dim3(320);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = (cudaStream_t)cuda_stream;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)p.o.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = p.o.split > 1 ? 1 : 0;
-        e = cudaLaunchKernelEx(&cfg, mxfp_product_kernel, ma, mb, p);
-    }
-    if (e != cudaSuccess) { cudaGetLastError(); return PAC_ERR_CUDA; }
-    return PAC_OK;
+    if (launch_product(device, (cudaStream_t)cuda_stream, dev_a_codes, M, dev_b_codes, K, p) == cudaSuccess) return PAC_OK;
+    cudaGetLastError();
+    return PAC_ERR_CUDA;
 }
 
 // ---------------------------------------------------------------------------

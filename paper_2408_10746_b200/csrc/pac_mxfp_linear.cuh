@@ -42,6 +42,7 @@ struct MxOut {
     int nt;                                                 // tokens per tile, a multiple of 16
     int split;                                              // CTAs of a cluster that share a tile's reduction
     int n_acc;                                              // accumulators of nt columns
+    int terms;                                              // y is the sum of so many rows M apart (1: as it is)
 };
 struct MlParams {
     MxOut o;
@@ -72,14 +73,38 @@ __device__ __forceinline__ uint32_t lds8(uint32_t a) {
     return v;
 }
 
+__device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+template <int RANKS, typename Cluster>
+__device__ __forceinline__ float4 sum_ranks(Cluster& cluster, float4* part, int i) {
+    float4 u[RANKS];
+#pragma unroll
+    for (int k = 0; k < RANKS; ++k) u[k] = cluster.map_shared_rank(part, k)[i];
+#pragma unroll
+    for (int k = 1; k < RANKS; ++k) u[0] = add4(u[0], u[k]);
+    return u[0];
+}
+
+// A column of up to 16 tokens.
+template <typename T>
+__device__ __forceinline__ void mx_store16(T* y, long long ldy, int n, const float (&v)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        if (e < n) {
+            if constexpr (sizeof(T) == 4) y[e * ldy] = v[e];
+            else y[e * ldy] = __float2bfloat16(v[e]);
+        }
+    }
+}
 // Accumulators -> y, by all threads of the CTA.  A lane is an output column and an accumulator column a token, so a warp
 // stores 32 neighbours of a row of y; warps 2-9, two per quadrant of lanes, share the tokens.  A tile whose reduction is
 // split goes through shared memory and is added up by the cluster, rank by rank.  `used`: accumulators that some step has
-// written; `last`: the last one has been written in any case.
+// written; `last`: the last one has been written in any case.  last_word(token, column, sum) is what is stored of shared sums.
+template <typename Last>
 __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, unsigned char* smem, uint32_t accf, volatile int* abort_flag, int wt, int t0,
-                                          int rank, int used, bool last) {
+                                          int rank, int used, bool last, Last last_word) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n_tok = min(o.nt, o.M - t0);
+    const bool shared = o.split > 1 || o.terms > 1;
     if (warp >= 2 && warp < 10) {
         const bool ok = mbar_wait_uniform(accf, 0, abort_flag, nullptr);
         if (!ok) drain_after_abort(abort_flag);              // copies in flight land before their memory is written again
@@ -87,55 +112,78 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
         const int q = warp & 3, half = (warp - 2) >> 2;
         const int col = wt * 128 + q * 32 + lane;
         const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16);
-        float* part = reinterpret_cast<float*>(smem);
+        float* part = reinterpret_cast<float*>(smem) + q * 32 + lane;
         const float bad = __uint_as_float(0x7fffffffu);      // a wait that ran out leaves NaN, not a wrong number
+        const int most = min(o.n_acc, used);
         for (int c0 = half * 16; c0 < o.nt; c0 += 32) {
-            float v[16];
+            float v[16], w[16];
             tmem_ld16(taddr + c0, v);
             tmem_ld_wait();
-            for (int a = 1; a < o.n_acc; ++a) {
-                if (a >= used && !(last && a == o.n_acc - 1)) continue;
-                float w[16];
+            for (int a = 1; a < most; ++a) {
                 tmem_ld16(taddr + a * o.nt + c0, w);
                 tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) v[e] += w[e];
             }
+            if (last && most < o.n_acc) {
+                tmem_ld16(taddr + (o.n_acc - 1) * o.nt + c0, w);
+                tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if (!ok) v[e] = bad;
-                if (o.split > 1) {
-                    part[(c0 + e) * 128 + q * 32 + lane] = v[e];
-                } else if (c0 + e < n_tok && col < o.cols) {
-                    const long long at = (long long)(t0 + c0 + e) * o.ldy + col;
-                    if (o.y_f32) static_cast<float*>(o.y)[at] = v[e];
-                    else static_cast<bf16*>(o.y)[at] = __float2bfloat16(v[e]);
-                }
+                for (int e = 0; e < 16; ++e) v[e] += w[e];
+            }
+            if (!ok) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = bad;
+            }
+            if (shared) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) part[(c0 + e) * 128] = v[e];
+            } else if (col < o.cols) {
+                if (o.y_f32) mx_store16(static_cast<float*>(o.y) + (long long)(t0 + c0) * o.ldy + col, o.ldy, n_tok - c0, v);
+                else mx_store16(static_cast<bf16*>(o.y) + (long long)(t0 + c0) * o.ldy + col, o.ldy, n_tok - c0, v);
             }
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (o.split > 1) {
-        namespace cg = cooperative_groups;
-        cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();
-        const float* part = reinterpret_cast<const float*>(smem);
-        const int threads = (int)blockDim.x;
-        // tokens in turn over the ranks
-        const int mine = rank < n_tok ? (n_tok - rank + o.split - 1) / o.split : 0;
-        for (int i = threadIdx.x; i < mine * 128; i += threads) {
-            const int c = (i >> 7) * o.split + rank, n = i & 127, col = wt * 128 + n;
-            float v = 0.f;
-            for (int k = 0; k < o.split; ++k) v += cluster.map_shared_rank(part, k)[c * 128 + n];
-            if (col < o.cols) {
-                const long long at = (long long)(t0 + c) * o.ldy + col;
-                if (o.y_f32) static_cast<float*>(o.y)[at] = v;
-                else static_cast<bf16*>(o.y)[at] = __float2bfloat16(v);
-            }
+    if (!shared) return;
+    // groups of four columns of a token, 32 to a token
+    float4* part = reinterpret_cast<float4*>(smem);
+    const int groups = n_tok * 32;
+    if (o.terms > 1) {
+        // the smallest terms first
+        for (int i = threadIdx.x; i < groups; i += blockDim.x) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 12
+            for (int t = o.terms - 1; t >= 0; --t) v = add4(v, part[t * o.M * 32 + i]);
+            part[i] = v;
         }
-        cluster.sync();                                      // nobody leaves while its partial sums are still read
     }
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    if (o.split > 1) cluster.sync();
+    else __syncthreads();
+    const int g0 = (int)((long long)groups * rank / o.split), g1 = (int)((long long)groups * (rank + 1) / o.split);
+    for (int i = g0 + (int)threadIdx.x; i < g1; i += (int)blockDim.x) {
+        float4 v;
+        switch (o.split) {                                   // all ranks' parts are asked for before the first is added
+            case 2: v = sum_ranks<2>(cluster, part, i); break;
+            case 4: v = sum_ranks<4>(cluster, part, i); break;
+            case 8: v = sum_ranks<8>(cluster, part, i); break;
+            default: v = part[i];
+        }
+        const int c = i >> 5, col = wt * 128 + (i & 31) * 4;
+        const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (col + e >= o.cols) continue;
+            const long long at = (long long)(t0 + c) * o.ldy + col + e;
+            const float y = last_word(t0 + c, col + e, w[e]);
+            if (o.y_f32) static_cast<float*>(o.y)[at] = y;
+            else static_cast<bf16*>(o.y)[at] = __float2bfloat16(y);
+        }
+    }
+    if (o.split > 1) cluster.sync();                         // nobody leaves while its partial sums are still read
 }
 
 // Eight values of a row of x from element `at` on (0 where `have` runs out).
@@ -158,7 +206,7 @@ __device__ __forceinline__ void ml_load8(const float* p, bool vec, int have, flo
 // Warps: 0 copies, 1 MMAs, 2-9 convert W and store y, 10-13 (not ML_X_TMA) bring in x.
 template <bool GRAD, int XMODE>
 __global__ void __launch_bounds__(XMODE == ML_X_TMA ? 320 : 448, 1)
-mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x, const MlParams p) {
+mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ MlParams p) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     constexpr int TERMS = XMODE == ML_X_F32 ? 3 : 1;
@@ -365,7 +413,7 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
         }
     }
 
-    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, 2 * (kt1 - kt0), TERMS == 3);
+    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, 2 * (kt1 - kt0), TERMS == 3, [](int, int, float v) { return v; });
     drain_after_abort(abort_flag);
     if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
 }

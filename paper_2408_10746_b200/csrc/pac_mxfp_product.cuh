@@ -12,7 +12,9 @@ namespace pac {
 
 constexpr int MP_BK = 256, MP_MAX_STAGES = 8;
 constexpr uint32_t MP_W_BYTES = 128 * 128;
-constexpr uint32_t MP_SF_COL = 384;                          // scales in tensor memory: two sets of up to 24 columns from here on
+constexpr uint32_t MP_SF_COLS = 24;                          // scales in tensor memory: two sets of up to 24 columns behind the accumulators
+// Tokens that are not in 4 bits, a few of them (pac_mxfp_linear): as sums of MS_TERMS matrices in MXFP4, see split_mxfp_kernel.
+constexpr int MS_TERMS = 12, MS_MOST_TOKENS = 16;
 
 struct MpParams {
     MxOut o;
@@ -21,6 +23,11 @@ struct MpParams {
     int steps;                                              // ceil(K / 256)
     int stages;
     uint32_t x_bytes, stage_bytes;
+    uint32_t tmem_cols, sf_col;
+    bool after;                                             // launched ahead of the end of the kernel that writes A
+    // sums of terms: what a result that is not a number is formed from again
+    const void* x; long long ldx; int x_f32; int K;
+    const unsigned char* b_codes;
 };
 
 // D[tmem] (+)= A B with one scale per 32 values of a row; sf: tensor-memory addresses of the scales.
@@ -43,8 +50,23 @@ __device__ __forceinline__ uint32_t instr_desc_mxf4(int N, uint32_t half) {
     return (half << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | (1u << 27) | (half << 29);
 }
 
+// A block of x with an infinity or a NaN has no terms but a scale that is not a number, so every sum that it enters comes out
+// as NaN: such a result is formed value by value from x itself (rare, and slow).
+__device__ __noinline__ float ms_redo(const MpParams& p, int m, int col) {
+    const unsigned char* codes = p.b_codes + (long long)col * mx_row_bytes(p.K);
+    float y = 0.f;
+    for (int k = 0; k < p.K; ++k) {
+        const uint32_t c = (codes[k >> 1] >> (4 * (k & 1))) & 15u, mag = c & 7u;
+        const uint32_t s = p.b_scales[((long long)(col / MX_TILE) * p.pieces + k / MX_TILE) * MX_SCALE_PIECE + mx_scale_at((uint32_t)col % MX_TILE, (uint32_t)(k % MX_TILE) / MX_BLOCK)];
+        const float v = (mag < 2u ? 0.5f * (float)mag : __uint_as_float((mag + 252u) << 22)) * mx_scale_f32(s);
+        const float x = p.x_f32 ? static_cast<const float*>(p.x)[m * p.ldx + k] : __bfloat162float(static_cast<const bf16*>(p.x)[m * p.ldx + k]);
+        y = fmaf(x, c & 8u ? -v : v, y);
+    }
+    return y;
+}
+
 // Warps: 0 copies, 1 scales and MMAs, 2-9 store y.
-__global__ void __launch_bounds__(320, 1) mxfp_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MpParams p) {
+__global__ void __launch_bounds__(320, 2) mxfp_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MpParams p) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     __shared__ __align__(8) unsigned long long bars[2 * MP_MAX_STAGES + 1];
@@ -57,7 +79,7 @@ __global__ void __launch_bounds__(320, 1) mxfp_product_kernel(const __grid_const
     const int k0 = (int)((long long)p.steps * rank / p.o.split), k1 = (int)((long long)p.steps * (rank + 1) / p.o.split);
     const uint32_t ring0 = smem_u32(smem);
     // pieces of scales that the tile's tokens lie in (t0 is a multiple of 128); past the last row there are none
-    const int t_tiles = (int)min((long long)(p.o.nt + 127) / 128, ((long long)p.o.M - t0 + 127) / 128);
+    const int t_tiles = (int)min((long long)(p.o.nt + 127) / 128, ((long long)p.o.M * p.o.terms - t0 + 127) / 128);
 
     if (threadIdx.x == 0) {
         abort_sh = 0;
@@ -67,7 +89,7 @@ __global__ void __launch_bounds__(320, 1) mxfp_product_kernel(const __grid_const
         tma_prefetch_desc(&map_a);
         tma_prefetch_desc(&map_b);
     }
-    if (warp == 1) { tmem_alloc(smem_u32(&tmem_base_sh), 512u); tmem_relinquish(); }
+    if (warp == 1) { tmem_alloc(smem_u32(&tmem_base_sh), p.tmem_cols); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -77,18 +99,34 @@ __global__ void __launch_bounds__(320, 1) mxfp_product_kernel(const __grid_const
     const uint32_t sf_at = MP_W_BYTES + p.x_bytes;
 
     if (warp == 0) {
-        uint32_t s = 0, ph = 1;
-        for (int k = k0; k < k1; ++k) {
+        const uint32_t bytes = MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (1 + t_tiles);
+        auto load_b = [&](int k, uint32_t s) {
+            const uint32_t bar = full0 + 8 * s, dst = ring0 + s * p.stage_bytes;
+            mbar_expect_tx(bar, bytes);
+            ml_tma_2d(dst, &map_b, bar, k * 128, wt * 128);
+            bulk_load_1d(dst + sf_at, p.b_scales + ((long long)wt * p.pieces + 2 * k) * MX_SCALE_PIECE, 2 * MX_SCALE_PIECE, bar);
+        };
+        auto load_a = [&](int k, uint32_t s) {
+            const uint32_t bar = full0 + 8 * s, dst = ring0 + s * p.stage_bytes;
+            ml_tma_2d(dst + MP_W_BYTES, &map_a, bar, k * 128, t0);
+            for (int i = 0; i < t_tiles; ++i)
+                bulk_load_1d(dst + sf_at + 2 * MX_SCALE_PIECE * (1 + i), p.a_scales + ((long long)(t0 / 128 + i) * p.pieces + 2 * k) * MX_SCALE_PIECE,
+                             2 * MX_SCALE_PIECE, bar);
+        };
+        // the frozen matrix does not wait for the kernel before: its tiles of the first round come in meanwhile
+        const int first = min(p.stages, k1 - k0);
+        if (elect_one()) {
+            for (int i = 0; i < first; ++i) load_b(k0 + i, (uint32_t)i);
+            if (p.after) pdl_wait();
+            for (int i = 0; i < first; ++i) load_a(k0 + i, (uint32_t)i);
+        }
+        __syncwarp();
+        uint32_t s = 0, ph = 0;
+        for (int k = k0 + first; k < k1; ++k) {
             if (!mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
             if (elect_one()) {
-                const uint32_t bar = full0 + 8 * s, dst = ring0 + s * p.stage_bytes;
-                mbar_expect_tx(bar, MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (1 + t_tiles));
-                ml_tma_2d(dst, &map_b, bar, k * 128, wt * 128);
-                ml_tma_2d(dst + MP_W_BYTES, &map_a, bar, k * 128, t0);
-                bulk_load_1d(dst + sf_at, p.b_scales + ((long long)wt * p.pieces + 2 * k) * MX_SCALE_PIECE, 2 * MX_SCALE_PIECE, bar);
-                for (int i = 0; i < t_tiles; ++i)
-                    bulk_load_1d(dst + sf_at + 2 * MX_SCALE_PIECE * (1 + i), p.a_scales + ((long long)(t0 / 128 + i) * p.pieces + 2 * k) * MX_SCALE_PIECE,
-                                 2 * MX_SCALE_PIECE, bar);
+                load_b(k, s);
+                load_a(k, s);
             }
             __syncwarp();
             if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
@@ -102,7 +140,7 @@ __global__ void __launch_bounds__(320, 1) mxfp_product_kernel(const __grid_const
             tc_fence_after();
             if (elect_one()) {
                 const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
-                const uint32_t sf = tmem_base + MP_SF_COL + (i & 1) * 32u;   // copies and MMAs of one thread take effect in order
+                const uint32_t sf = tmem_base + p.sf_col + (i & 1) * MP_SF_COLS;   // copies and MMAs of one thread take effect in order
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {                // 128 values of K: one word of scales per row
                     tmem_copy_scales(sf + c * 4, f0 + off + c * (MX_SCALE_PIECE >> 4));
@@ -122,29 +160,90 @@ __global__ void __launch_bounds__(320, 1) mxfp_product_kernel(const __grid_const
         if (elect_one()) umma_commit(accf);
         __syncwarp();
     }
-    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, k1 - k0, false);
+    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, k1 - k0, false,
+              [&](int m, int col, float v) { return p.o.terms > 1 && v != v ? ms_redo(p, m, col) : v; });
     drain_after_abort(abort_flag);
-    if (warp == 1) tmem_dealloc(tmem_base, 512u);
+    if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
 }
 
+// Sizes and split of a call; terms > 1: A is a sum of so many matrices of o.M rows each, below one another.
 inline bool mp_plan(MpParams& p, int K, int sms) {
-    const int cap = p.o.y_f32 ? 128 : 256;
+    const int rows = p.o.M * p.o.terms, cap = p.o.y_f32 && p.o.terms == 1 ? 128 : 256;
     // several token tiles begin at multiples of 128, where the pieces of scales do
-    p.o.nt = p.o.M <= cap ? (p.o.M + 15) / 16 * 16 : cap;
-    const int tok_tiles = (p.o.M + p.o.nt - 1) / p.o.nt;
+    p.o.nt = rows <= cap ? (rows + 15) / 16 * 16 : cap;
+    const int tok_tiles = (rows + p.o.nt - 1) / p.o.nt;
     const long long wts = ((long long)p.o.cols + 127) / 128, ctas = wts * tok_tiles;
     p.steps = (int)(((long long)K + MP_BK - 1) / MP_BK);
-    p.o.n_acc = 384 / p.o.nt < 3 ? 384 / p.o.nt : 3;
+    p.x_bytes = (uint32_t)p.o.nt * 128u;
+    p.stage_bytes = MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (uint32_t)(1 + (p.o.nt + 127) / 128);
+    p.stage_bytes = (p.stage_bytes + 1023u) / 1024u * 1024u;
+    // up to 192 tokens two CTAs share an SM: half the tensor memory and half the shared memory each
+    const bool two = p.o.nt <= 192;
+    const int acc_cols = two ? 208 : 464;
+    p.tmem_cols = two ? 256 : 512;
+    p.sf_col = (uint32_t)acc_cols;
+    p.o.n_acc = acc_cols / p.o.nt < 3 ? acc_cols / p.o.nt : 3;
     p.o.split = 1;
     while (p.o.split < 8 && p.o.split * 2 <= p.steps && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
     // fp32 results: at most 128 additions (of 64 products each) into an accumulator
     while (p.o.y_f32 && p.o.split < 8 && p.o.split * 2 <= p.steps && (long long)p.steps * 4 > 128LL * p.o.n_acc * p.o.split) p.o.split *= 2;
-    p.x_bytes = (uint32_t)p.o.nt * 128u;
-    p.stage_bytes = MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (uint32_t)(1 + (p.o.nt + 127) / 128);
-    p.stage_bytes = (p.stage_bytes + 1023u) / 1024u * 1024u;
-    p.stages = (int)(ML_SMEM_MOST / p.stage_bytes);
+    p.stages = (int)((two ? (ML_SMEM_MOST - 4096) / 2 : ML_SMEM_MOST) / p.stage_bytes);
     if (p.stages > MP_MAX_STAGES) p.stages = MP_MAX_STAGES;
     return wts * p.o.split <= 0x7fffffffLL && tok_tiles <= 65535;
+}
+// Shared memory of a CTA: the ring, and room for partial sums where they go through it.
+inline size_t mp_smem(const MpParams& p) {
+    const size_t ring = (size_t)p.stages * p.stage_bytes, part = p.o.split > 1 || p.o.terms > 1 ? (size_t)p.o.nt * 512 : 0;
+    return 1024 + (ring > part ? ring : part);
+}
+
+// x [M][K], bf16 or fp32, as a sum of MS_TERMS matrices in MXFP4, term t in rows t M .. t M + M - 1: the first is x rounded, each
+// next one is what the ones before it leave, rounded with a scale of its own.  Every term takes at least two bits off the
+// largest of a block's 32 remainders (a value of [4, 8) units is at most 2 off, 1 up to 6), 2.6 of them on the average, so
+// the sum is x to 2^-24 of the largest of the 32: exact for bf16 values within 2^16 of each other.  With it the products of a
+// few tokens are block-scaled products of the codes of W as they are: nothing converts W, whose bytes are the floor.
+// A warp takes a block, a lane a value.
+template <typename T>
+__global__ void __launch_bounds__(256) split_mxfp_kernel(const T* __restrict__ x, int M, int K, long long ldx, unsigned char* __restrict__ codes,
+                                                         unsigned char* __restrict__ scales) {
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, pieces = mx_col_pieces(K), blocks = pieces * 4;
+    const long long row_bytes = mx_row_bytes(K);
+    const int id = (int)((blockIdx.x * blockDim.x + threadIdx.x) >> 5), m = id / blocks, b = id - m * blocks;
+    if (m >= M) return;
+    const int col = b * MX_BLOCK + lane;
+    float r = col < K ? to_f32(x[m * ldx + col]) : 0.f;
+    const bool finite = !__any_sync(0xffffffffu, !(fabsf(r) < __uint_as_float(0x7f800000u)));
+    if (!finite) r = 0.f;
+#pragma unroll 1
+    for (int t = 0; t < MS_TERMS; ++t) {
+        const uint32_t ex = __reduce_max_sync(0xffffffffu, __float_as_uint(r) & 0x7fffffffu) >> 23;
+        const uint32_t s = ex > 2u ? ex - 2u : 0u;
+        uint32_t c;
+        asm("{\n .reg .b8 b0;\n cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n mov.b32 %0, {b0, b0, b0, b0};\n}"
+            : "=r"(c) : "f"(r * __uint_as_float((254u - s) << 23)), "f"(0.f));
+        c &= 15u;
+        const uint32_t mag = c & 7u;
+        const float v = mag < 2u ? 0.5f * (float)mag : __uint_as_float((mag + 252u) << 22);
+        r -= (c & 8u ? -v : v) * mx_scale_f32(s);            // exact: both are multiples of r's last bit, and the difference is smaller
+        uint32_t w = c << (4 * (lane & 7));
+        w |= __shfl_xor_sync(0xffffffffu, w, 1);
+        w |= __shfl_xor_sync(0xffffffffu, w, 2);
+        w |= __shfl_xor_sync(0xffffffffu, w, 4);
+        const int row = t * M + m;
+        if ((lane & 7) == 0 && b * 16 < row_bytes) *reinterpret_cast<uint32_t*>(codes + row * row_bytes + b * 16 + (lane >> 1)) = w;
+        if (lane == 0) scales[((long long)(row / MX_TILE) * pieces + b / 4) * MX_SCALE_PIECE + mx_scale_at((uint32_t)(row % MX_TILE), (uint32_t)b % 4u)] = finite || t ? (unsigned char)s : 255;
+    }
+}
+// The workspace that holds the terms.
+struct MsSpace { long long codes, scales, bytes; };
+inline MsSpace ms_space(int M, int K) {
+    MsSpace w;
+    const long long rows = (long long)M * MS_TERMS;
+    w.codes = 0;
+    w.scales = (rows * mx_row_bytes(K) + 255) / 256 * 256;
+    w.bytes = w.scales + (rows + MX_TILE - 1) / MX_TILE * mx_col_pieces(K) * (long long)MX_SCALE_PIECE;
+    return w;
 }
 
 }  // namespace pac

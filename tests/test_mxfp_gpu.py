@@ -174,17 +174,65 @@ def test_not_a_number_stays_in_its_row_or_column(which):
         assert y[[7, 9]].isnan().all() and y[:7].isfinite().all() and y[10:].isfinite().all()
 
 
+@pytest.mark.parametrize("xt", ["bf16", "f32"])
+def test_few_tokens_with_values_that_are_not_finite_and_of_all_sizes(xt):
+    """Up to 16 tokens x is a sum of twelve 4-bit matrices: to 2^-24 of the largest of 32 neighbours; infinities and NaN as ever."""
+    import paper_2408_10746_b200 as pac
+    codes, scales, w = matrix(300, 1100, 21)
+    g = torch.Generator().manual_seed(3)
+    x = (torch.randn(16, 1100, generator=g) * torch.exp2(torch.randint(-30, 30, (16, 1100), generator=g).float())).to(TYPES[xt]).cuda()
+    x[3] = 0
+    x[5, 7:40] = 0
+    near = host(x)
+    top = np.abs(np.pad(near, ((0, 0), (0, 20)))).reshape(16, 35, 32).max(2).repeat(32, 1)[:, :1100]
+    y = pac.mxfp_linear(x, codes, scales, torch.float32)
+    tol = bound(near @ w.T, np.abs(near) @ np.abs(w.T), 1100 / 64 + 16 + 12, torch.float32) + 2.0 ** -24 * (top @ np.abs(w.T))
+    assert (np.abs(host(y) - near @ w.T) <= tol).all()
+    x[2, 500], x[7, 0], x[9, 1099] = float("inf"), float("nan"), -float("inf")
+    x[9, 3] = float("inf")
+    got, want = host(pac.mxfp_linear(x, codes, scales, torch.float32)), (host(x)[:, None, :] * w[None]).sum(2)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want))
+    assert np.array_equal(np.sign(got[np.isinf(got)]), np.sign(want[np.isinf(want)]))
+    assert np.array_equal(got[[0, 1, 3, 4, 5, 6, 8]], host(y)[[0, 1, 3, 4, 5, 6, 8]])
+
+
+def test_few_tokens_without_a_workspace_and_with_one_too_small():
+    import paper_2408_10746_b200 as pac
+    lib = pac.load_library()
+    codes, scales, w = matrix(130, 200, 2)
+    x, y = torch.randn(3, 200, device="cuda"), torch.empty(3, 130, device="cuda")
+    n = lib.pac_mxfp_linear_workspace(3, 200)
+    assert n > 0 and lib.pac_mxfp_linear_workspace(17, 200) == 0
+    space = torch.empty(n, dtype=torch.uint8, device="cuda")
+    call = lambda at, size: lib.pac_mxfp_linear(0, torch.cuda.current_stream().cuda_stream, x.data_ptr(), 0, 3, 200, codes.data_ptr(), scales.data_ptr(), 130, 200,  # noqa: E731
+                                                y.data_ptr(), 0, 130, at, size)
+    assert call(space.data_ptr(), n - 1) == 1 and call(space.data_ptr() + 16, n) == 1
+    ref, size = host(x) @ w.T, np.abs(host(x)) @ np.abs(w.T)
+    for at, have in ((None, 0), (space.data_ptr(), n)):
+        y.fill_(float("nan"))
+        assert call(at, have) == 0
+        assert (np.abs(host(y) - ref) <= bound(ref, size, 200 / 16 + 16, torch.float32)).all()
+
+
 def test_filling_bytes_of_the_scales_do_not_matter_to_linear():
     import paper_2408_10746_b200 as pac
-    codes, scales, _ = matrix(100, 72, 4)
+    codes, scales, w = matrix(100, 72, 4)
     x, dy = torch.randn(9, 72, device="cuda"), torch.randn(9, 100, device="cuda")
     want = pac.mxfp_linear(x, codes, scales), pac.mxfp_linear_grad(dy, codes, scales, 72)
     row = 32 * torch.arange(4, device="cuda")[None, :, None] + torch.arange(32, device="cuda")[:, None, None]
     block = torch.arange(4, device="cuda")[None, None, :]
     scales[0, 0] = torch.where((row >= 100) | (block >= 3), 255, scales[0, 0])
     scales[0, 1] = 255
-    assert torch.equal(pac.mxfp_linear(x, codes, scales), want[0])
+    # (few tokens: a sum that a filling byte has made NaN is formed again, by 72 fused operations in fp32: 72 roundings of 2^-24
+    # of the sum of magnitudes, less than the (72 / 16 + 16) 2^-22 of bound())
+    ref, size = host(x) @ w.T, np.abs(host(x)) @ np.abs(w.T)
+    for y in (want[0], pac.mxfp_linear(x, codes, scales)):
+        assert (np.abs(host(y) - ref) <= bound(ref, size, 72 / 16 + 16, torch.float32)).all()
     assert torch.equal(pac.mxfp_linear_grad(dy, codes, scales, 72), want[1])
+    more = torch.randn(20, 72, device="cuda")
+    got = pac.mxfp_linear(more, codes, scales)
+    scales[0, 1] = 0
+    assert torch.equal(pac.mxfp_linear(more, codes, scales), got) and got.isfinite().all()
 
 
 @pytest.mark.parametrize("s", [0, 1, 60, 200, 240])
