@@ -527,7 +527,7 @@ def _rows(t, name: str):
     rows, cols = t.shape
     if cols < 1:
         _refuse(f"{name} has at least one column")
-    step, ld = t.stride(1), t.stride(0)
+    ld, step = t.stride()
     if cols > 1 and step != 1 and rows:
         _refuse(f"{name}: elements of a row are consecutive")
     if rows <= 1:
@@ -551,11 +551,11 @@ def _mxfp(codes, scales, cols: int, device=None):
     if not (codes.is_cuda and scales.is_cuda and codes.dtype is torch.uint8 and scales.dtype is torch.uint8 and codes.dim() == 2
             and codes.is_contiguous() and scales.is_contiguous() and cols > 0):
         _refuse("codes and scales are contiguous CUDA uint8 tensors")
-    rows = codes.shape[0]
-    want = mxfp_shapes(rows, cols)
-    if codes.shape != want[0] or scales.shape != want[1]:
-        _refuse(f"{rows} x {cols} values have codes and scales of shapes {want}, not {tuple(codes.shape)} and {tuple(scales.shape)}")
-    if codes.device != scales.device or (device is not None and codes.device != device):
+    rows, width = codes.shape
+    if width != 16 * ((cols + 31) // 32) or scales.shape != ((rows + 127) // 128, 2 * ((cols + 255) // 256), 32, 4, 4):
+        _refuse(f"{rows} x {cols} values have codes and scales of shapes {mxfp_shapes(rows, cols)}, not {tuple(codes.shape)} and {tuple(scales.shape)}")
+    at = codes.device
+    if at != scales.device or (device is not None and at != device):
         _refuse("all tensors are on one device")
     return rows
 
@@ -564,7 +564,7 @@ def _out(out, rows: int, cols: int, dtype, device):
     """The tensor that receives a result, made here when the caller gives none."""
     import torch
     if out is None:
-        return torch.empty((rows, cols), dtype=dtype, device=device), cols
+        return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device), cols
     if out.shape != (rows, cols) or out.dtype != dtype or out.device != device:
         _refuse(f"out is {rows} x {cols} {dtype} on {device}")
     return out, _rows(out, "out")[2]
@@ -576,12 +576,16 @@ def quantize_mxfp(x, codes=None, scales=None):
     import torch
     rows, cols, ld = _rows(x, "x")
     device, dtype = x.device, _dtype(x.dtype)
-    if codes is None or scales is None:
+    if codes is None and scales is None:
+        width, tiles, pieces = 16 * ((cols + 31) // 32), (rows + 127) // 128, 2 * ((cols + 255) // 256)
+        codes = torch.empty_strided((rows, width), (width, 1), dtype=torch.uint8, device=device)
+        scales = torch.empty_strided((tiles, pieces, 32, 4, 4), (512 * pieces, 512, 16, 4, 1), dtype=torch.uint8, device=device)
+    else:
         shapes = mxfp_shapes(rows, cols)
         codes = torch.empty(shapes[0], dtype=torch.uint8, device=device) if codes is None else codes
         scales = torch.empty(shapes[1], dtype=torch.uint8, device=device) if scales is None else scales
-    if _mxfp(codes, scales, cols, device) != rows:
-        _refuse(f"codes have {rows} rows")
+        if _mxfp(codes, scales, cols, device) != rows:
+            _refuse(f"codes have {rows} rows")
     index = device.index
     st = load_library().pac_quantize_mxfp(index, _stream(index), x.data_ptr(), dtype, rows, cols, ld, codes.data_ptr(), scales.data_ptr())
     if st != 0:
@@ -622,9 +626,8 @@ def mxfp_linear(x, codes, scales, dtype=None, out=None):
     lib = load_library()
     if M > MXFP_FEW_TOKENS or M < 1:
         return _mxfp_linear(lib.pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out, None, 0)
-    import torch
     n = lib.pac_mxfp_linear_workspace(M, K)
-    space = torch.empty(n, dtype=torch.uint8, device=x.device)
+    space = codes.new_empty(n)
     return _mxfp_linear(lib.pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out, space.data_ptr(), n)
 
 

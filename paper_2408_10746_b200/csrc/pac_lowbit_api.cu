@@ -7,6 +7,7 @@
 #include "pac_adamw_tensors.cuh"
 #include "pac_mxfp.cuh"
 #include "pac_mxfp_linear.cuh"
+#include "pac_mxfp_pair.cuh"
 #include "pac_mxfp_product.cuh"
 
 using namespace pac;
@@ -139,6 +140,27 @@ cudaError_t few_tokens(int device, cudaStream_t st, const void* x, int x_dtype, 
     return e != cudaSuccess ? e : launch_product(device, st, space + w.codes, M * MS_TERMS, codes, K, p);
 }
 
+// Many tokens: pairs of CTAs (pac_mxfp_pair.cuh).  x in bf16, its rows on 16-byte boundaries.
+template <bool GRAD>
+cudaError_t launch_pair(int device, cudaStream_t st, const CUtensorMap& codes, const CUtensorMap& x, const MrParams& p, int sms) {
+    const auto kernel = mxfp_linear_pair_kernel<GRAD>;
+    static OptedIn done;
+    const cudaError_t e = opt_in(done, (const void*)kernel, device);
+    if (e != cudaSuccess) return e;
+    const long long units = (long long)p.w_units * p.t_units;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2u * (unsigned)(units < sms / 2 ? units : sms / 2));
+    cfg.blockDim = dim3(MR_THREADS);
+    cfg.dynamicSmemBytes = MR_SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, codes, x, p);
+}
+
 pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x_dtype, int M, long long ldx, const unsigned char* codes,
                        const unsigned char* scales, int N, int K, void* y, int y_dtype, long long ldy, void* space = nullptr, long long space_bytes = 0) {
     const int red = grad ? N : K, out_cols = grad ? K : N;
@@ -162,9 +184,23 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     const bool rows16 = aligned(x, 16) && (ldx * (long long)dtype_size(x_dtype)) % 16 == 0;
     const int mode = x_dtype == PAC_F32 ? ML_X_F32 : rows16 ? ML_X_TMA : ML_X_BF16;
     p.x_vec = rows16;
-    if (!ml_plan(p, mode == ML_X_F32, mode != ML_X_TMA, sm_count(device))) return PAC_ERR_UNSUPPORTED;
+    const int sms = sm_count(device);
     CUtensorMap mc, mx;
-    if (!map_2d(&mc, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, mx_row_bytes(K), N, mx_row_bytes(K), 64, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) return PAC_ERR_CUDA;
+    if (!map_2d(&mc, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, mx_row_bytes(K), N, mx_row_bytes(K), 64, 128, CU_TENSOR_MAP_SWIZZLE_64B)) return PAC_ERR_CUDA;
+    const long long w_tiles = (out_cols + 127LL) / 128, units = (w_tiles + 1) / 2 * ((M + 255LL) / 256);
+    // pairs where their tiles fill more than half of the SMs; fp32 results up to where two accumulators take 128 additions each
+    if (mode == ML_X_TMA && M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (!p.o.y_f32 || red <= 4096)) {
+        MrParams r = {};
+        r.y = y; r.ldy = ldy; r.y_f32 = p.o.y_f32; r.scales = scales;
+        r.M = M; r.cols = out_cols; r.red = red; r.pieces = p.pieces; r.red_tiles = (int)((red + 127LL) / 128);
+        r.w_tiles = (int)w_tiles; r.w_units = (int)((w_tiles + 1) / 2); r.t_units = (int)((M + 255LL) / 256);
+        r.n_acc = p.o.y_f32 ? 2 : 1;
+        if (!map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, red, M, ldx * 2, ML_BK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) return PAC_ERR_CUDA;
+        if ((grad ? launch_pair<true>(device, st, mc, mx, r, sms) : launch_pair<false>(device, st, mc, mx, r, sms)) == cudaSuccess) return PAC_OK;
+        cudaGetLastError();
+        return PAC_ERR_CUDA;
+    }
+    if (!ml_plan(p, mode == ML_X_F32, mode != ML_X_TMA, sms)) return PAC_ERR_UNSUPPORTED;
     mx = mc;
     if (mode == ML_X_TMA && !map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, red, M, ldx * 2, ML_BK, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B)) return PAC_ERR_CUDA;
     cudaError_t e;

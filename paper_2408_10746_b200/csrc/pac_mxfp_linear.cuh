@@ -67,9 +67,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
     uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
 }
 
@@ -203,6 +203,53 @@ __device__ __forceinline__ void ml_load8(const float* p, bool vec, int have, flo
     u[0] = make_float4(f[0], f[1], f[2], f[3]); u[1] = make_float4(f[4], f[5], f[6], f[7]);
 }
 
+// Codes -> a K step's bf16 tile.  Four warps take a step (the eight in turn, so that a warp has two steps' time for the
+// waits and fences of one); a thread takes two blocks of 32.  Forward: the step's 64 columns of row `t`; backward: half of
+// the 128 columns of row h * 64 + t / 2 (the other 64 are another thread's).  The copy of the codes swizzles their 16-byte
+// blocks over 512 bytes, and odd threads begin with their second block backward, so that neither the reads nor the writes
+// of eight neighbours meet in a bank.
+template <bool GRAD>
+struct MlBlocks {
+    uint4 c[2];
+    uint32_t f[2];
+    __device__ __forceinline__ static int row(int t, int h) { return GRAD ? h * 64 + (t >> 1) : t; }
+    __device__ __forceinline__ static int block(int t, int h, int i) { return GRAD ? (t & 1) * 2 + (i ^ (t & 1)) : h * 2 + i; }
+    // src: a piece of codes and its scales; kt: the piece along the reduction of length red
+    __device__ __forceinline__ void load(uint32_t src, int t, int h, int kt, int red) {
+        const int r = row(t, h);
+        const uint32_t scales = lds32(src + 128 * 64 + mx_scale_at((uint32_t)r, 0u));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int b = block(t, h, i);
+            c[i] = lds128(src + r * 64 + (((uint32_t)b ^ (((uint32_t)r >> 1) & 3u)) << 4));
+            // beyond the reduction the codes are 0 and the scale is whatever fills the piece: it must not be a NaN
+            const bool in = GRAD ? kt * 128 + r < red : kt * 128 + b * 32 < red;
+            f[i] = in ? mx_scale_bf16x2((scales >> (8 * b)) & 255u) : 0u;
+        }
+    }
+    __device__ __forceinline__ void convert(uint32_t (&o)[2][4][4]) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                mx_bf16x8(w[j], o[i][j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][j][e] = mul_bf16x2(o[i][j][e], f[i]);
+            }
+        }
+    }
+    __device__ __forceinline__ static void store(uint32_t tile, int t, int h, const uint32_t (&o)[2][4][4]) {
+        const uint32_t r = (uint32_t)(GRAD ? t >> 1 : t), dst = tile + (GRAD ? (uint32_t)(t & 1) * 8192u : 0u) + r * 128u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t chunk0 = (uint32_t)(block(t, h, i) & 1) * 4u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sts128(dst + (((chunk0 + j) ^ (r & 7u)) << 4), make_uint4(o[i][j][0], o[i][j][1], o[i][j][2], o[i][j][3]));
+        }
+    }
+};
+
 // Warps: 0 copies, 1 MMAs, 2-9 convert W and store y, 10-13 (not ML_X_TMA) bring in x.
 template <bool GRAD, int XMODE>
 __global__ void __launch_bounds__(XMODE == ML_X_TMA ? 320 : 448, 1)
@@ -227,7 +274,7 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
         abort_sh = 0;
         for (int s = 0; s < p.stages; ++s) {
             mbar_init(xfull0 + 8 * s, XMODE == ML_X_TMA ? 1 : ML_X_WARPS);
-            mbar_init(afull0 + 8 * s, ML_CONV_WARPS);
+            mbar_init(afull0 + 8 * s, ML_CONV_WARPS / 2);
             mbar_init(empty0 + 8 * s, 1);
         }
         for (int s = 0; s < p.code_stages; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, ML_CONV_WARPS); }
@@ -305,51 +352,24 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
         if (elect_one()) umma_commit(accf);
         __syncwarp();
     } else if (warp < 2 + ML_CONV_WARPS) {
-        const int t = threadIdx.x - 64;
-        uint32_t cs = 0, cph = 0, s = 0, ph = 1;
-        bool ok = true;
-        // this thread's block of 32: forward row t / 2, block t % 2 of the step's 64 columns; backward row t / 4 of the
-        // step's 64 rows, block t % 4 of the 128 columns
-        const int r = GRAD ? t >> 2 : t >> 1, b = GRAD ? t & 3 : t & 1;
-        const uint32_t dst0 = GRAD ? (uint32_t)((b >> 1) * 8192 + r * 128) : (uint32_t)(r * 128);
-        const uint32_t chunk0 = GRAD ? (uint32_t)(b & 1) * 4u : (uint32_t)b * 4u, swz = (uint32_t)r & 7u;
-        for (int kt = kt0; kt < kt1 && ok; ++kt) {
-            ok = mbar_wait_uniform(cfull0 + 8 * cs, cph, abort_flag, nullptr);
-            if (!ok) break;
-            const uint32_t src = codes0 + cs * ML_CODE_BYTES;
-            uint4 c[2];
-            uint32_t f[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = GRAD ? h * 64 + r : r, blk = GRAD ? b : h * 2 + b;
-                c[h] = lds128(src + row * 64 + blk * 16);
-                // beyond the reduction the codes are 0 and the scale is whatever fills the piece: it must not be a NaN
-                const bool in = GRAD ? kt * 128 + row < p.red : kt * 128 + blk * 32 < p.red;
-                f[h] = in ? mx_scale_bf16x2(lds8(src + 128 * 64 + mx_scale_at((uint32_t)row, (uint32_t)blk))) : 0u;
-            }
+        const int h = (warp - 2) >> 2, t = threadIdx.x - 64 - h * 128;
+        uint32_t cs = 0, cph = 0, s = (uint32_t)h, ph = 1;
+        for (int kt = kt0; kt < kt1; ++kt) {
+            if (!mbar_wait_uniform(cfull0 + 8 * cs, cph, abort_flag, nullptr)) break;
+            MlBlocks<GRAD> w;
+            w.load(codes0 + cs * ML_CODE_BYTES, t, h, kt, p.red);
+            uint32_t o[2][4][4];
+            w.convert(o);
             __syncwarp();
             if (lane == 0) mbar_arrive(cempty0 + 8 * cs);
             if (++cs == (uint32_t)p.code_stages) { cs = 0; cph ^= 1u; }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t o[4][4];
-                const uint32_t w[4] = {c[h].x, c[h].y, c[h].z, c[h].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    mx_bf16x8(w[j], o[j]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[j][e] = mul_bf16x2(o[j][e], f[h]);
-                }
-                ok = ok && mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr);
-                if (!ok) break;
-                const uint32_t dst = ring0 + s * p.stage_bytes + dst0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sts128(dst + ((chunk0 + j) ^ swz) * 16u, make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]));
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(afull0 + 8 * s);
-                if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
-            }
+            if (!mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
+            w.store(ring0 + s * p.stage_bytes, t, h, o);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(afull0 + 8 * s);
+            s += 2;
+            if (s >= (uint32_t)p.stages) { s = (uint32_t)h; ph ^= 1u; }
         }
     } else {
         // x by threads: 16-byte chunks of the swizzled tile, the next step's values on their way while this step waits for its stage
@@ -441,7 +461,7 @@ inline bool ml_plan(MlParams& p, bool f32_terms, bool by_threads, int sms) {
     p.code_stages = p.o.nt > 128 ? 3 : 6;
     const size_t room = ML_SMEM_MOST - (size_t)p.code_stages * ((ML_CODE_BYTES + 127) / 128 * 128);
     p.stages = (int)(room / p.stage_bytes);
-    if (p.stages > ML_MAX_STAGES) p.stages = ML_MAX_STAGES;
+    p.stages = (p.stages > ML_MAX_STAGES ? ML_MAX_STAGES : p.stages) & ~1;      // even: a group of converters has every other one
     p.code_at = (uint32_t)p.stages * p.stage_bytes;
     return (long long)wts * p.o.split <= 0x7fffffffLL && tok_tiles <= 65535;
 }

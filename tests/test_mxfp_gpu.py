@@ -129,6 +129,15 @@ def test_linear_and_its_gradient_against_64_bits(grad, M, N, K, xt, yt):
     check_linear(grad, M, N, K, xt, yt)
 
 
+@pytest.mark.parametrize("M,N,K", [(1000, 3000, 136), (520, 8200, 300), (2049, 1300, 520), (700, 2600, 128)])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("yt", ["bf16", "f32"])
+def test_many_tokens(grad, M, N, K, yt):
+    """Tiles of pairs of CTAs: several to a pair, odd ones at every edge."""
+    check_linear(grad, M, *((K, N) if grad else (N, K)), "bf16", yt, pad=0 if K % 8 == 0 and N % 8 == 0 else 4)
+    check_linear(grad, M, *((K, N) if grad else (N, K)), "bf16", yt, pad=8, out_pad=3)
+
+
 @pytest.mark.parametrize("grad", [False, True])
 @pytest.mark.parametrize("xt,yt,pad,offset,out_pad", [("bf16", "f32", 8, 0, 3), ("bf16", "bf16", 3, 0, 8), ("bf16", "bf16", 8, 1, 0), ("f32", "bf16", 4, 0, 5),
                                                       ("f32", "f32", 0, 1, 0), ("f32", "f32", 3, 3, 7)])
