@@ -123,12 +123,12 @@ def load_library() -> C.CDLL:
     lib.pac_quantize_mxfp.argtypes = [I, P, P, I, LL, I, LL, P, P]
     lib.pac_dequantize_mxfp.argtypes = [I, P, P, P, LL, I, P, I, LL]
     lib.pac_mxfp_linear.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL, P, LL]
-    lib.pac_mxfp_linear_grad.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL]
+    lib.pac_mxfp_linear_grad.argtypes = [I, P, P, I, I, LL, P, P, I, I, P, I, LL, P, LL]
     lib.pac_mxfp_product.argtypes = [I, P, P, P, I, P, P, I, I, P, I, LL]
     lib.pac_adamw_tensors.argtypes = [I, P, C.POINTER(_AdamWTensor), I, I, C.POINTER(_AdamW), LL, P, F, C.c_uint]
     for name in ("pac_quantize_mxfp", "pac_dequantize_mxfp", "pac_mxfp_linear", "pac_mxfp_linear_grad", "pac_mxfp_product", "pac_adamw_tensors"):
         getattr(lib, name).restype = I
-    lib.pac_mxfp_linear_workspace.argtypes = [I, I]
+    lib.pac_mxfp_linear_workspace.argtypes = [P, I, I, LL, I, I]
     lib.pac_mxfp_linear_workspace.restype = LL
     lib.pac_last_error.argtypes = [P]
     lib.pac_last_error.restype = C.c_char_p
@@ -537,9 +537,6 @@ def _rows(t, name: str):
     return rows, cols, ld
 
 
-MXFP_FEW_TOKENS = 16          # calls of so many tokens go by way of a workspace
-
-
 def mxfp_shapes(rows: int, cols: int):
     """Shapes of the codes and of the scales (both uint8) of a rows x cols matrix."""
     return (rows, 16 * ((cols + 31) // 32)), ((rows + 127) // 128, 2 * ((cols + 255) // 256), 32, 4, 4)
@@ -607,11 +604,14 @@ def dequantize_mxfp(codes, scales, cols: int, dtype=None, out=None):
     return out
 
 
-def _mxfp_linear(call, x, M: int, ld: int, codes, scales, N: int, K: int, cols: int, dtype, out, *space):
+def _mxfp_linear(call, lib, x, M: int, ld: int, codes, scales, N: int, K: int, grad: bool, dtype, out):
     dtype = dtype or (out.dtype if out is not None else x.dtype)
-    device, xt, yt = x.device, _dtype(x.dtype), _dtype(dtype)
-    out, ldo = _out(out, M, cols, dtype, device)
-    st = call(device.index, _stream(device.index), x.data_ptr(), xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K, out.data_ptr(), yt, ldo, *space)
+    device, xt, yt, at = x.device, _dtype(x.dtype), _dtype(dtype), x.data_ptr()
+    out, ldo = _out(out, M, K if grad else N, dtype, device)
+    n = lib.pac_mxfp_linear_workspace(at, xt, M, ld, N if grad else K, grad)
+    space = codes.new_empty(n) if n else None
+    st = call(device.index, _stream(device.index), at, xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K, out.data_ptr(), yt, ldo,
+              space.data_ptr() if n else None, n)
     if st != 0:
         raise PacError(st, f"{call.__name__} failed")
     return out
@@ -624,11 +624,7 @@ def mxfp_linear(x, codes, scales, dtype=None, out=None):
     if N < 1:
         _refuse("W has at least one row")
     lib = load_library()
-    if M > MXFP_FEW_TOKENS or M < 1:
-        return _mxfp_linear(lib.pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out, None, 0)
-    n = lib.pac_mxfp_linear_workspace(M, K)
-    space = codes.new_empty(n)
-    return _mxfp_linear(lib.pac_mxfp_linear, x, M, ld, codes, scales, N, K, N, dtype, out, space.data_ptr(), n)
+    return _mxfp_linear(lib.pac_mxfp_linear, lib, x, M, ld, codes, scales, N, K, False, dtype, out)
 
 
 def mxfp_linear_grad(dy, codes, scales, cols: int, dtype=None, out=None):
@@ -636,7 +632,8 @@ def mxfp_linear_grad(dy, codes, scales, cols: int, dtype=None, out=None):
     M, N, ld = _rows(dy, "dy")
     if _mxfp(codes, scales, cols, dy.device) != N:
         _refuse(f"dy has {N} columns, one per row of W")
-    return _mxfp_linear(load_library().pac_mxfp_linear_grad, dy, M, ld, codes, scales, N, cols, cols, dtype, out)
+    lib = load_library()
+    return _mxfp_linear(lib.pac_mxfp_linear_grad, lib, dy, M, ld, codes, scales, N, cols, True, dtype, out)
 
 
 def mxfp_product(a_codes, a_scales, b_codes, b_scales, cols: int, dtype=None, out=None):

@@ -71,17 +71,16 @@ cudaError_t opt_in(OptedIn& done, const void* kernel, int device) {
     return e;
 }
 
-template <bool GRAD, int XMODE>
+template <bool GRAD, int TERMS>
 cudaError_t launch_linear(int device, cudaStream_t st, const CUtensorMap& codes, const CUtensorMap& x, const MlParams& p) {
-    const auto kernel = mxfp_linear_kernel<GRAD, XMODE>;
-    const size_t smem = 1024 + p.code_at + (size_t)p.code_stages * ML_CODE_BYTES;
+    const auto kernel = mxfp_linear_kernel<GRAD, TERMS>;
     static OptedIn done;
-    cudaError_t e = opt_in(done, (const void*)kernel, device);
+    const cudaError_t e = opt_in(done, (const void*)kernel, device);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(((p.o.cols + 127LL) / 128) * p.o.split), (unsigned)((p.o.M + p.o.nt - 1) / p.o.nt));
-    cfg.blockDim = dim3(XMODE == ML_X_TMA ? 320 : 448);
-    cfg.dynamicSmemBytes = smem;
+    cfg.blockDim = dim3(32 * (2 + ML_CONV_WARPS));
+    cfg.dynamicSmemBytes = 1024 + p.code_at + (size_t)p.code_stages * ML_CODE_BYTES;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -161,57 +160,70 @@ cudaError_t launch_pair(int device, cudaStream_t st, const CUtensorMap& codes, c
     return cudaLaunchKernelEx(&cfg, kernel, codes, x, p);
 }
 
+bool few(bool grad, int M) { return !grad && M <= MS_MOST_TOKENS; }
+// Rows that TMA boxes can read as they are.
+bool boxes(const void* x, int dtype, long long ldx) { return dtype == PAC_BF16 && aligned(x, 16) && ldx % 8 == 0; }
+long long linear_space(bool grad, const void* x, int dtype, int M, long long ldx, int red) {
+    if (few(grad, M)) return ms_space(M, red).bytes;
+    return boxes(x, dtype, ldx) ? 0 : (dtype == PAC_F32 ? 6LL : 2LL) * M * pack_columns(red);
+}
+
 pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x_dtype, int M, long long ldx, const unsigned char* codes,
-                       const unsigned char* scales, int N, int K, void* y, int y_dtype, long long ldy, void* space = nullptr, long long space_bytes = 0) {
+                       const unsigned char* scales, int N, int K, void* y, int y_dtype, long long ldy, void* space, long long space_bytes) {
     const int red = grad ? N : K, out_cols = grad ? K : N;
     if (M < 0 || !matrix_ok(codes, scales, N, K) || !dtype_ok(x_dtype) || !dtype_ok(y_dtype)) return PAC_ERR_INVALID_ARG;
     if (M == 0) return PAC_OK;
-    if (!x || !y || ldx < red || ldy < out_cols || M > 0x7fffff00) return PAC_ERR_INVALID_ARG;
+    if (!x || !y || ldx < red || ldy < out_cols || M > 0x0fffff00) return PAC_ERR_INVALID_ARG;
     if (!aligned(x, dtype_size(x_dtype)) || !aligned(y, dtype_size(y_dtype))) return PAC_ERR_INVALID_ARG;
+    const long long need = linear_space(grad, x, x_dtype, M, ldx, red);
+    if (need > 0 && (!space || !aligned(space, 256) || space_bytes < need)) return PAC_ERR_INVALID_ARG;
     OnDevice on(device);
     if (!on.ok) return PAC_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)stream;
-    if (!grad && space && M <= MS_MOST_TOKENS) {
-        if (!aligned(space, 256) || space_bytes < ms_space(M, K).bytes) return PAC_ERR_INVALID_ARG;
-        if (few_tokens(device, st, x, x_dtype, M, ldx, codes, scales, N, K, y, y_dtype, ldy, (unsigned char*)space) == cudaSuccess) return PAC_OK;
+    auto status = [](cudaError_t e) {
+        if (e == cudaSuccess) return PAC_OK;
         cudaGetLastError();
         return PAC_ERR_CUDA;
+    };
+    if (few(grad, M)) return status(few_tokens(device, st, x, x_dtype, M, ldx, codes, scales, N, K, y, y_dtype, ldy, (unsigned char*)space));
+    const int sms = sm_count(device), terms = x_dtype == PAC_F32 ? 3 : 1;
+    const bool y_f32 = y_dtype == PAC_F32;
+    long long x_cols = red, x_pitch = ldx;
+    if (need > 0) {
+        x_cols = x_pitch = pack_columns(red);
+        const long long want = ((long long)M * x_cols / 8 + 255) / 256, most = (long long)sms * 32;
+        const unsigned grid = (unsigned)(want < most ? want : most);
+        const bool vec = aligned(x, 16) && ldx % 4 == 0;
+        if (x_dtype == PAC_F32) pack_tokens_kernel<float><<<grid, 256, 0, st>>>((const float*)x, M, red, ldx, vec, (bf16*)space);
+        else pack_tokens_kernel<bf16><<<grid, 256, 0, st>>>((const bf16*)x, M, red, ldx, vec, (bf16*)space);
+        if (cudaGetLastError() != cudaSuccess) return PAC_ERR_CUDA;
+        x = space;
+    }
+    CUtensorMap mc, mx;
+    if (!map_2d(&mc, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, mx_row_bytes(K), N, mx_row_bytes(K), 64, 128, CU_TENSOR_MAP_SWIZZLE_64B)) return PAC_ERR_CUDA;
+    auto map_x = [&](int box_rows) {
+        return map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, x_cols, (long long)terms * M, x_pitch * 2, ML_BK, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+    };
+    const long long w_tiles = (out_cols + 127LL) / 128, units = (w_tiles + 1) / 2 * ((M + 255LL) / 256);
+    // pairs where their tiles fill more than half of the SMs; fp32 results up to where two accumulators take 128 additions each
+    if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (!y_f32 || red <= 4096)) {
+        MrParams r = {};
+        r.y = y; r.ldy = ldy; r.y_f32 = y_f32; r.scales = scales;
+        r.M = M; r.cols = out_cols; r.red = red; r.pieces = mx_col_pieces(K); r.red_tiles = (int)((red + 127LL) / 128);
+        r.w_tiles = (int)w_tiles; r.w_units = (int)((w_tiles + 1) / 2); r.t_units = (int)((M + 255LL) / 256);
+        r.n_acc = y_f32 ? 2 : 1;
+        r.terms = terms; r.x_rows = M;
+        if (!map_x(128)) return PAC_ERR_CUDA;
+        return status(grad ? launch_pair<true>(device, st, mc, mx, r, sms) : launch_pair<false>(device, st, mc, mx, r, sms));
     }
     MlParams p = {};
     p.o.terms = 1;
-    p.x = x; p.ldx = ldx; p.scales = scales; p.o.y = y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32;
-    p.o.M = M; p.o.cols = out_cols; p.red = red; p.pieces = mx_col_pieces(K);
-    const bool rows16 = aligned(x, 16) && (ldx * (long long)dtype_size(x_dtype)) % 16 == 0;
-    const int mode = x_dtype == PAC_F32 ? ML_X_F32 : rows16 ? ML_X_TMA : ML_X_BF16;
-    p.x_vec = rows16;
-    const int sms = sm_count(device);
-    CUtensorMap mc, mx;
-    if (!map_2d(&mc, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, mx_row_bytes(K), N, mx_row_bytes(K), 64, 128, CU_TENSOR_MAP_SWIZZLE_64B)) return PAC_ERR_CUDA;
-    const long long w_tiles = (out_cols + 127LL) / 128, units = (w_tiles + 1) / 2 * ((M + 255LL) / 256);
-    // pairs where their tiles fill more than half of the SMs; fp32 results up to where two accumulators take 128 additions each
-    if (mode == ML_X_TMA && M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (!p.o.y_f32 || red <= 4096)) {
-        MrParams r = {};
-        r.y = y; r.ldy = ldy; r.y_f32 = p.o.y_f32; r.scales = scales;
-        r.M = M; r.cols = out_cols; r.red = red; r.pieces = p.pieces; r.red_tiles = (int)((red + 127LL) / 128);
-        r.w_tiles = (int)w_tiles; r.w_units = (int)((w_tiles + 1) / 2); r.t_units = (int)((M + 255LL) / 256);
-        r.n_acc = p.o.y_f32 ? 2 : 1;
-        if (!map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, red, M, ldx * 2, ML_BK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) return PAC_ERR_CUDA;
-        if ((grad ? launch_pair<true>(device, st, mc, mx, r, sms) : launch_pair<false>(device, st, mc, mx, r, sms)) == cudaSuccess) return PAC_OK;
-        cudaGetLastError();
-        return PAC_ERR_CUDA;
-    }
-    if (!ml_plan(p, mode == ML_X_F32, mode != ML_X_TMA, sms)) return PAC_ERR_UNSUPPORTED;
-    mx = mc;
-    if (mode == ML_X_TMA && !map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, red, M, ldx * 2, ML_BK, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B)) return PAC_ERR_CUDA;
-    cudaError_t e;
-    if (grad)
-        e = mode == ML_X_TMA ? launch_linear<true, ML_X_TMA>(device, st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<true, ML_X_BF16>(device, st, mc, mx, p)
-                                                                                                 : launch_linear<true, ML_X_F32>(device, st, mc, mx, p);
-    else
-        e = mode == ML_X_TMA ? launch_linear<false, ML_X_TMA>(device, st, mc, mx, p) : mode == ML_X_BF16 ? launch_linear<false, ML_X_BF16>(device, st, mc, mx, p)
-                                                                                                  : launch_linear<false, ML_X_F32>(device, st, mc, mx, p);
-    if (e != cudaSuccess) { cudaGetLastError(); return PAC_ERR_CUDA; }
-    return PAC_OK;
+    p.scales = scales; p.o.y = y; p.o.ldy = ldy; p.o.y_f32 = y_f32;
+    p.o.M = M; p.o.cols = out_cols; p.red = red; p.pieces = mx_col_pieces(K); p.x_rows = M;
+    if (!ml_plan(p, terms == 3, sms)) return PAC_ERR_UNSUPPORTED;
+    if (!map_x(p.o.nt)) return PAC_ERR_CUDA;
+    if (grad) return status(terms == 3 ? launch_linear<true, 3>(device, st, mc, mx, p) : launch_linear<true, 1>(device, st, mc, mx, p));
+    return status(terms == 3 ? launch_linear<false, 3>(device, st, mc, mx, p) : launch_linear<false, 1>(device, st, mc, mx, p));
 }
 
 }  // namespace
@@ -255,12 +267,15 @@ extern "C" pac_status pac_mxfp_linear(int device, void* cuda_stream, const void*
     return mxfp_linear(false, device, cuda_stream, dev_x, x_dtype, M, ldx, dev_codes, dev_scales, N, K, dev_y, y_dtype, ldy, dev_workspace, workspace_bytes);
 }
 
-extern "C" long long pac_mxfp_linear_workspace(int M, int K) { return M < 1 || M > MS_MOST_TOKENS || K < 1 || K > 0x7fffff00 ? 0 : ms_space(M, K).bytes; }
+extern "C" long long pac_mxfp_linear_workspace(const void* dev_x, int x_dtype, int M, long long ldx, int reduction, int grad) {
+    if (M < 1 || M > 0x0fffff00 || reduction < 1 || reduction > 0x7fffff00 || !dtype_ok(x_dtype)) return 0;
+    return linear_space(grad != 0, dev_x, x_dtype, M, ldx, reduction);
+}
 
 extern "C" pac_status pac_mxfp_linear_grad(int device, void* cuda_stream, const void* dev_dy, int dy_dtype, int M, long long lddy,
                                            const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_dx, int dx_dtype,
-                                           long long lddx) {
-    return mxfp_linear(true, device, cuda_stream, dev_dy, dy_dtype, M, lddy, dev_codes, dev_scales, N, K, dev_dx, dx_dtype, lddx);
+                                           long long lddx, void* dev_workspace, long long workspace_bytes) {
+    return mxfp_linear(true, device, cuda_stream, dev_dy, dy_dtype, M, lddy, dev_codes, dev_scales, N, K, dev_dx, dx_dtype, lddx, dev_workspace, workspace_bytes);
 }
 
 extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsigned char* dev_a_codes, const unsigned char* dev_a_scales, int M,

@@ -27,12 +27,11 @@
 namespace pac {
 
 constexpr int ML_BK = 64;                                   // reduction elements per stage
-constexpr int ML_CONV_WARPS = 8, ML_X_WARPS = 4;
+constexpr int ML_CONV_WARPS = 16;                            // in groups of four, each with every fourth step
 constexpr uint32_t ML_A_BYTES = 128 * ML_BK * 2;
 constexpr uint32_t ML_CODE_BYTES = 128 * 64 + MX_SCALE_PIECE;
 constexpr int ML_MAX_STAGES = 8, ML_MAX_CODES = 8;
 constexpr size_t ML_SMEM_MOST = 232448 - 1024 - 512;
-enum { ML_X_TMA = 0, ML_X_BF16 = 1, ML_X_F32 = 2 };         // how x reaches shared memory: TMA boxes, or threads (any alignment, or fp32)
 
 // What becomes of a product's accumulators (the block-scaled product's as well).
 struct MxOut {
@@ -46,7 +45,6 @@ struct MxOut {
 };
 struct MlParams {
     MxOut o;
-    const void* x; long long ldx;                           // ML_X_BF16, ML_X_F32
     const unsigned char* scales;
     int red;                                                // length of the reduction: K, or N with GRAD
     int pieces;                                             // pieces of scales per row tile
@@ -54,7 +52,7 @@ struct MlParams {
     int stages, code_stages;
     uint32_t stage_bytes, code_at;                          // bytes per stage; offset of the ring of codes
     uint32_t tmem_cols;
-    bool x_vec;                                             // rows of x start on 16-byte boundaries
+    int x_rows;                                             // rows of a term of x
 };
 
 __device__ __forceinline__ void ml_tma_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
@@ -186,25 +184,54 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
     if (o.split > 1) cluster.sync();                         // nobody leaves while its partial sums are still read
 }
 
-// Eight values of a row of x from element `at` on (0 where `have` runs out).
-__device__ __forceinline__ void ml_load8(const bf16* p, bool vec, int have, uint4& u) {
-    if (vec && have >= 8) { u = *reinterpret_cast<const uint4*>(p); return; }
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
+// x as TMA boxes can read it: TERMS matrices [rows][16-byte rows of whole 128-column pieces] in bf16, below one another.  A bf16 x
+// whose rows do not begin on 16-byte boundaries is copied; an fp32 x becomes three bf16 terms that add up to it exactly.
+__host__ __device__ inline int pack_columns(int red) { return (red + 127) / 128 * 128; }
+template <typename T>
+__global__ void __launch_bounds__(256) pack_tokens_kernel(const T* __restrict__ x, int M, int red, long long ldx, bool vec, bf16* __restrict__ out) {
+    const int cols = pack_columns(red), groups = cols / 8;
+    const long long items = (long long)M * groups, term = (long long)M * cols;
+    for (long long it = (long long)blockIdx.x * blockDim.x + threadIdx.x; it < items; it += (long long)gridDim.x * blockDim.x) {
+        const long long m = it / groups;
+        const int c0 = (int)(it - m * groups) * 8;
+        const T* p = x + m * ldx + c0;
+        float v[8];
+        if (sizeof(T) == 4 && vec && c0 + 8 <= red) {
+            const float4 a = *reinterpret_cast<const float4*>(p), b = *(reinterpret_cast<const float4*>(p) + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < have) w[e >> 1] |= (uint32_t)__bfloat16_as_ushort(p[e]) << (16 * (e & 1));
-    u = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void ml_load8(const float* p, bool vec, int have, float4 (&u)[2]) {
-    if (vec && have >= 8) { u[0] = *reinterpret_cast<const float4*>(p); u[1] = *reinterpret_cast<const float4*>(p + 4); return; }
-    float f[8];
+            for (int e = 0; e < 8; ++e) v[e] = c0 + e < red ? to_f32(p[e]) : 0.f;
+        }
+        uint32_t h[4], l[4], t[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = e < have ? p[e] : 0.f;
-    u[0] = make_float4(f[0], f[1], f[2], f[3]); u[1] = make_float4(f[4], f[5], f[6], f[7]);
+        for (int e = 0; e < 4; ++e) {
+            h[e] = bf16_pair(v[2 * e], v[2 * e + 1]);
+            if constexpr (sizeof(T) == 4) {
+                float r[2];
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const float x1 = v[2 * e + f];
+                    const bool finite = fabsf(x1) < __uint_as_float(0x7f800000u);
+                    // the largest values round to an infinity: one step less; an infinity or a NaN is its own first term
+                    if (finite && ((h[e] >> (16 * f)) & 0x7fffu) == 0x7f80u) h[e] -= 1u << (16 * f);
+                    r[f] = finite ? x1 - __uint_as_float(f ? h[e] & 0xffff0000u : h[e] << 16) : 0.f;
+                }
+                l[e] = bf16_pair(r[0], r[1]);
+                t[e] = bf16_pair(r[0] - __uint_as_float(l[e] << 16), r[1] - __uint_as_float(l[e] & 0xffff0000u));
+            }
+        }
+        bf16* dst = out + m * cols + c0;
+        *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<uint4*>(dst + term) = make_uint4(l[0], l[1], l[2], l[3]);
+            *reinterpret_cast<uint4*>(dst + 2 * term) = make_uint4(t[0], t[1], t[2], t[3]);
+        }
+    }
 }
 
-// Codes -> a K step's bf16 tile.  Four warps take a step (the eight in turn, so that a warp has two steps' time for the
-// waits and fences of one); a thread takes two blocks of 32.  Forward: the step's 64 columns of row `t`; backward: half of
+// Codes -> a K step's bf16 tile.  Four warps take a step, the groups of four in turn, so that a warp has several steps' time
+// for the waits and fences of one; a thread takes two blocks of 32.  Forward: the step's 64 columns of row `t`; backward: half of
 // the 128 columns of row h * 64 + t / 2 (the other 64 are another thread's).  The copy of the codes swizzles their 16-byte
 // blocks over 512 bytes, and odd threads begin with their second block backward, so that neither the reads nor the writes
 // of eight neighbours meet in a bank.
@@ -250,13 +277,12 @@ struct MlBlocks {
     }
 };
 
-// Warps: 0 copies, 1 MMAs, 2-9 convert W and store y, 10-13 (not ML_X_TMA) bring in x.
-template <bool GRAD, int XMODE>
-__global__ void __launch_bounds__(XMODE == ML_X_TMA ? 320 : 448, 1)
+// Warps: 0 copies, 1 MMAs, 2-17 convert W, 2-9 store y.
+template <bool GRAD, int TERMS>
+__global__ void __launch_bounds__(32 * (2 + ML_CONV_WARPS), 1)
 mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ MlParams p) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    constexpr int TERMS = XMODE == ML_X_F32 ? 3 : 1;
     __shared__ __align__(8) unsigned long long bars[3 * ML_MAX_STAGES + 2 * ML_MAX_CODES + 1];
     __shared__ uint32_t tmem_base_sh;
     __shared__ int abort_sh;
@@ -267,21 +293,18 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
     const int rank = p.o.split > 1 ? (int)(blockIdx.x % p.o.split) : 0;
     const int wt = blockIdx.x / p.o.split, t0 = blockIdx.y * p.o.nt;
     const int kt0 = (int)((long long)p.red_tiles * rank / p.o.split), kt1 = (int)((long long)p.red_tiles * (rank + 1) / p.o.split);
+    const int steps = 2 * (kt1 - kt0);
     const uint32_t ring0 = smem_u32(smem), codes0 = ring0 + p.code_at;
     const uint32_t term_bytes = (uint32_t)p.o.nt * 128u;
 
     if (threadIdx.x == 0) {
         abort_sh = 0;
-        for (int s = 0; s < p.stages; ++s) {
-            mbar_init(xfull0 + 8 * s, XMODE == ML_X_TMA ? 1 : ML_X_WARPS);
-            mbar_init(afull0 + 8 * s, ML_CONV_WARPS / 2);
-            mbar_init(empty0 + 8 * s, 1);
-        }
-        for (int s = 0; s < p.code_stages; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, ML_CONV_WARPS); }
+        for (int s = 0; s < p.stages; ++s) { mbar_init(xfull0 + 8 * s, 1); mbar_init(afull0 + 8 * s, 4); mbar_init(empty0 + 8 * s, 1); }
+        for (int s = 0; s < p.code_stages; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, 8); }
         mbar_init(accf, 1);
         fence_mbar_init();
         tma_prefetch_desc(&map_codes);
-        if (XMODE == ML_X_TMA) tma_prefetch_desc(&map_x);
+        tma_prefetch_desc(&map_x);
     }
     if (warp == 1) { tmem_alloc(smem_u32(&tmem_base_sh), p.tmem_cols); tmem_relinquish(); }
     tc_fence_before();
@@ -305,17 +328,17 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
             }
             __syncwarp();
             if (++cs == (uint32_t)p.code_stages) { cs = 0; cph ^= 1u; }
-            if constexpr (XMODE == ML_X_TMA) {
-                for (int h = 0; h < 2 && ok; ++h) {
-                    ok = mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr);
-                    if (!ok) break;
-                    if (elect_one()) {
-                        mbar_expect_tx(xfull0 + 8 * s, term_bytes);
-                        ml_tma_2d(ring0 + s * p.stage_bytes + ML_A_BYTES, &map_x, xfull0 + 8 * s, kt * 128 + h * 64, t0);
-                    }
-                    __syncwarp();
-                    if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+            for (int h = 0; h < 2 && ok; ++h) {
+                ok = mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr);
+                if (!ok) break;
+                if (elect_one()) {
+                    mbar_expect_tx(xfull0 + 8 * s, TERMS * term_bytes);
+#pragma unroll
+                    for (int e = 0; e < TERMS; ++e)          // (rows of a tile past the last token may be another term's: no one stores them)
+                        ml_tma_2d(ring0 + s * p.stage_bytes + ML_A_BYTES + e * term_bytes, &map_x, xfull0 + 8 * s, kt * 128 + h * 64, e * p.x_rows + t0);
                 }
+                __syncwarp();
+                if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
             }
         }
     } else if (warp == 1) {
@@ -324,7 +347,7 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
         const uint64_t b0 = smem_desc_sw128(ring0 + ML_A_BYTES, 16, 1024);
         const uint64_t astep = GRAD ? 128u : 2u;             // 16 elements of the reduction further, in 16-byte units
         uint32_t s = 0, ph = 0, acc = 0;
-        const int steps = 2 * (kt1 - kt0), lead = TERMS == 1 ? p.o.n_acc : p.o.n_acc - 1;
+        const int lead = TERMS == 1 ? p.o.n_acc : p.o.n_acc - 1;
         bool ok = true;
         for (int i = 0; i < steps && ok; ++i) {
             ok = mbar_wait_uniform(xfull0 + 8 * s, ph, abort_flag, nullptr) && mbar_wait_uniform(afull0 + 8 * s, ph, abort_flag, nullptr);
@@ -351,96 +374,37 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
         }
         if (elect_one()) umma_commit(accf);
         __syncwarp();
-    } else if (warp < 2 + ML_CONV_WARPS) {
-        const int h = (warp - 2) >> 2, t = threadIdx.x - 64 - h * 128;
-        uint32_t cs = 0, cph = 0, s = (uint32_t)h, ph = 1;
-        for (int kt = kt0; kt < kt1; ++kt) {
+    } else {
+        constexpr int GROUPS = ML_CONV_WARPS / 4;
+        const int g = (warp - 2) >> 2, h = g & 1, t = (threadIdx.x - 64) & 127;
+        uint32_t cs = (uint32_t)g >> 1, cph = 0, s = (uint32_t)g, ph = 1;       // (there are at least two pieces and four steps in either ring)
+        for (int i = g; i < steps; i += GROUPS) {
             if (!mbar_wait_uniform(cfull0 + 8 * cs, cph, abort_flag, nullptr)) break;
             MlBlocks<GRAD> w;
-            w.load(codes0 + cs * ML_CODE_BYTES, t, h, kt, p.red);
+            w.load(codes0 + cs * ML_CODE_BYTES, t, h, kt0 + (i >> 1), p.red);
             uint32_t o[2][4][4];
             w.convert(o);
             __syncwarp();
             if (lane == 0) mbar_arrive(cempty0 + 8 * cs);
-            if (++cs == (uint32_t)p.code_stages) { cs = 0; cph ^= 1u; }
+            cs += GROUPS / 2;
+            if (cs >= (uint32_t)p.code_stages) { cs -= (uint32_t)p.code_stages; cph ^= 1u; }
             if (!mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
             w.store(ring0 + s * p.stage_bytes, t, h, o);
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(afull0 + 8 * s);
-            s += 2;
-            if (s >= (uint32_t)p.stages) { s = (uint32_t)h; ph ^= 1u; }
-        }
-    } else {
-        // x by threads: 16-byte chunks of the swizzled tile, the next step's values on their way while this step waits for its stage
-        const int t = threadIdx.x - 64 - 32 * ML_CONV_WARPS;
-        constexpr int PER = XMODE == ML_X_F32 ? 4 : 8;       // chunks per thread: 64 tokens (fp32), 128 tokens
-        typedef typename std::conditional<XMODE == ML_X_F32, float, bf16>::type T;
-        uint32_t s = 0, ph = 1;
-        const int steps = 2 * (kt1 - kt0), chunks = p.o.nt * 8;
-        uint4 nb[PER];
-        float4 nf[PER][2];
-        auto fetch = [&](int i) {
-            const int k0 = kt0 * 128 + i * 64;
-#pragma unroll
-            for (int q = 0; q < PER; ++q) {
-                const int id = q * 128 + t, row = t0 + (id >> 3), at = k0 + (id & 7) * 8;
-                const int have = (id < chunks && row < p.o.M) ? p.red - at : 0;
-                const T* src = static_cast<const T*>(p.x) + (long long)row * p.ldx + at;
-                if constexpr (XMODE == ML_X_F32) {
-                    if (have > 0) ml_load8(src, p.x_vec, have, nf[q]);
-                    else nf[q][0] = nf[q][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-                } else {
-                    if (have > 0) ml_load8(src, p.x_vec, have, nb[q]);
-                    else nb[q] = make_uint4(0u, 0u, 0u, 0u);
-                }
-            }
-        };
-        if (steps > 0) fetch(0);
-        for (int i = 0; i < steps; ++i) {
-            uint4 u[PER][TERMS];
-#pragma unroll
-            for (int q = 0; q < PER; ++q) {
-                if constexpr (XMODE == ML_X_F32) {
-                    uint32_t h[4], m[4], l[4];
-                    split3_pair(nf[q][0].x, nf[q][0].y, h[0], m[0], l[0]);
-                    split3_pair(nf[q][0].z, nf[q][0].w, h[1], m[1], l[1]);
-                    split3_pair(nf[q][1].x, nf[q][1].y, h[2], m[2], l[2]);
-                    split3_pair(nf[q][1].z, nf[q][1].w, h[3], m[3], l[3]);
-                    u[q][0] = make_uint4(h[0], h[1], h[2], h[3]);
-                    u[q][1] = make_uint4(m[0], m[1], m[2], m[3]);
-                    u[q][2] = make_uint4(l[0], l[1], l[2], l[3]);
-                } else {
-                    u[q][0] = nb[q];
-                }
-            }
-            if (i + 1 < steps) fetch(i + 1);
-            if (!mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
-            const uint32_t dst = ring0 + s * p.stage_bytes + ML_A_BYTES;
-#pragma unroll
-            for (int q = 0; q < PER; ++q) {
-                const int id = q * 128 + t;
-                if (id < chunks) {
-                    const uint32_t row = (uint32_t)id >> 3, at = row * 128u + (((uint32_t)id & 7u) ^ (row & 7u)) * 16u;
-#pragma unroll
-                    for (int e = 0; e < TERMS; ++e) sts128(dst + e * term_bytes + at, u[q][e]);
-                }
-            }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(xfull0 + 8 * s);
-            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+            s += GROUPS;
+            if (s >= (uint32_t)p.stages) { s = (uint32_t)g; ph ^= 1u; }
         }
     }
-
-    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, 2 * (kt1 - kt0), TERMS == 3, [](int, int, float v) { return v; });
+    mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, steps, TERMS == 3, [](int, int, float v) { return v; });
     drain_after_abort(abort_flag);
     if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
 }
 
 // Tile, split and rings of one call; false when the sizes do not fit the grid.
-inline bool ml_plan(MlParams& p, bool f32_terms, bool by_threads, int sms) {
-    const int cap = f32_terms ? 64 : by_threads || p.o.y_f32 ? 128 : 256;
+inline bool ml_plan(MlParams& p, bool f32_terms, int sms) {
+    const int cap = f32_terms ? 64 : p.o.y_f32 ? 128 : 256;
     const int tiles = (p.o.M + cap - 1) / cap;
     p.o.nt = ((p.o.M + tiles - 1) / tiles + 15) / 16 * 16;
     const int wts = (int)(((long long)p.o.cols + 127) / 128);
@@ -461,7 +425,7 @@ inline bool ml_plan(MlParams& p, bool f32_terms, bool by_threads, int sms) {
     p.code_stages = p.o.nt > 128 ? 3 : 6;
     const size_t room = ML_SMEM_MOST - (size_t)p.code_stages * ((ML_CODE_BYTES + 127) / 128 * 128);
     p.stages = (int)(room / p.stage_bytes);
-    p.stages = (p.stages > ML_MAX_STAGES ? ML_MAX_STAGES : p.stages) & ~1;      // even: a group of converters has every other one
+    p.stages = p.stages >= ML_MAX_STAGES ? ML_MAX_STAGES : 4;      // 4 or 8: a group of converters has every fourth
     p.code_at = (uint32_t)p.stages * p.stage_bytes;
     return (long long)wts * p.o.split <= 0x7fffffffLL && tok_tiles <= 65535;
 }

@@ -3,13 +3,14 @@
 // converted once per 256 tokens and a K step of 64 costs an SM 8192 conversions and 20 KB from L2 for 512 clocks of tensor work;
 // alone it would be the same conversions and 36 KB.  Persistent pairs; the accumulators of one tile are stored while the
 // next tile is computed (bf16 results), or both halves of tensor memory take turns within a tile (fp32 results: half the
-// additions into either).
+// additions into either).  An fp32 x comes as three bf16 terms and the reduction goes over W three times, the smallest term first: what
+// is cut off while the sums are small is smaller still.
 #pragma once
 #include "pac_mxfp_linear.cuh"
 
 namespace pac {
 
-constexpr int MR_STAGES = 6, MR_CODES = 3, MR_EPI_WARPS = 4, MR_THREADS = 32 * (2 + ML_CONV_WARPS + MR_EPI_WARPS);
+constexpr int MR_STAGES = 6, MR_CODES = 3, MR_CONV_WARPS = 8, MR_EPI_WARPS = 4, MR_THREADS = 32 * (2 + MR_CONV_WARPS + MR_EPI_WARPS);
 constexpr uint32_t MR_STAGE = 2 * ML_A_BYTES;
 constexpr size_t MR_SMEM = 1024 + (size_t)MR_STAGES * MR_STAGE + (size_t)MR_CODES * ML_CODE_BYTES;
 
@@ -20,6 +21,7 @@ struct MrParams {
     int w_tiles;                                            // 128-wide tiles of y's columns
     int w_units, t_units;                                   // pairs of them; tiles of 256 tokens
     int n_acc;                                              // accumulators per tile: 1 (two tiles in flight) or 2
+    int terms, x_rows;                                      // x is the sum of so many matrices of x_rows rows, the last ones (the small ones) first
 };
 
 __device__ __forceinline__ void mr_tma_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar_cluster, int c0, int c1) {
@@ -68,8 +70,8 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
 
     if (threadIdx.x == 0) {
         abort_sh = 0;
-        for (int s = 0; s < MR_STAGES; ++s) { mbar_init(xfull0 + 8 * s, 1); mbar_init(afull0 + 8 * s, ML_CONV_WARPS); mbar_init(empty0 + 8 * s, 1); }
-        for (int s = 0; s < MR_CODES; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, ML_CONV_WARPS); }
+        for (int s = 0; s < MR_STAGES; ++s) { mbar_init(xfull0 + 8 * s, 1); mbar_init(afull0 + 8 * s, MR_CONV_WARPS); mbar_init(empty0 + 8 * s, 1); }
+        for (int s = 0; s < MR_CODES; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, MR_CONV_WARPS); }
         for (int b = 0; b < 2; ++b) { mbar_init(accf0 + 8 * b, 1); mbar_init(acce0 + 8 * b, 2 * MR_EPI_WARPS); }
         fence_mbar_init();
         tma_prefetch_desc(&map_codes);
@@ -89,7 +91,7 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
         for (int u = unit0; u < units && ok; u += unit_step) {
             // an odd last tile has no partner: its codes lie outside (zeros), its scales are another tile's, nothing of it is stored
             const int wt = (u % p.w_units) * 2 + (int)rank, t0 = (u / p.w_units) * 256 + (int)rank * 128;
-            for (int kt = 0; kt < p.red_tiles && ok; ++kt) {
+            for (int i = 0, kt = 0, row = t0 + (p.terms - 1) * p.x_rows; i < p.terms * p.red_tiles && ok; ++i) {
                 ok = mbar_wait_uniform(cempty0 + 8 * cs, cph, abort_flag, nullptr);
                 if (!ok) break;
                 if (elect_one()) {
@@ -107,11 +109,12 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
                     if (!ok) break;
                     if (elect_one()) {
                         if (rank == 0) mbar_expect_tx(xfull0 + 8 * s, 2 * ML_A_BYTES);
-                        mr_tma_2d(ring0 + s * MR_STAGE + ML_A_BYTES, &map_x, mapa_shared(xfull0 + 8 * s, 0u), kt * 128 + h * 64, t0);
+                        mr_tma_2d(ring0 + s * MR_STAGE + ML_A_BYTES, &map_x, mapa_shared(xfull0 + 8 * s, 0u), kt * 128 + h * 64, row);
                     }
                     __syncwarp();
                     if (++s == MR_STAGES) { s = 0; ph ^= 1u; }
                 }
+                if (++kt == p.red_tiles) { kt = 0; row -= p.x_rows; }
             }
         }
     } else if (warp == 1) {
@@ -126,7 +129,7 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
                 ok = mr_wait(acce0 + 8 * buf, (use & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                const int steps = 2 * p.red_tiles;
+                const int steps = 2 * p.terms * p.red_tiles;
                 for (int i = 0; i < steps; ++i) {
                     ok = mr_wait(xfull0 + 8 * s, ph, abort_flag) && mr_wait(afull0 + 8 * s, ph, abort_flag);
                     if (!ok) break;
@@ -147,13 +150,13 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
                 __syncwarp();
             }
         }
-    } else if (warp < 2 + ML_CONV_WARPS) {
+    } else if (warp < 2 + MR_CONV_WARPS) {
         const int h = (warp - 2) >> 2, t = threadIdx.x - 64 - h * 128;
         uint32_t cs = 0, cph = 0, s = (uint32_t)h, ph = 1;
         const uint32_t afull_first = mapa_shared(afull0, 0u);
         bool ok = true;
         for (int u = unit0; u < units && ok; u += unit_step) {
-            for (int kt = 0; kt < p.red_tiles && ok; ++kt) {
+            for (int i = 0, kt = 0; i < p.terms * p.red_tiles && ok; ++i) {
                 ok = mbar_wait_uniform(cfull0 + 8 * cs, cph, abort_flag, nullptr);
                 if (!ok) break;
                 MlBlocks<GRAD> w;
@@ -171,6 +174,7 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
                 if (lane == 0) mr_arrive(afull_first + 8 * s);
                 s += 2;
                 if (s >= MR_STAGES) { s = (uint32_t)h; ph ^= 1u; }
+                if (++kt == p.red_tiles) kt = 0;
             }
         }
     } else {

@@ -131,11 +131,11 @@ def test_linear_and_its_gradient_against_64_bits(grad, M, N, K, xt, yt):
 
 @pytest.mark.parametrize("M,N,K", [(1000, 3000, 136), (520, 8200, 300), (2049, 1300, 520), (700, 2600, 128)])
 @pytest.mark.parametrize("grad", [False, True])
-@pytest.mark.parametrize("yt", ["bf16", "f32"])
-def test_many_tokens(grad, M, N, K, yt):
+@pytest.mark.parametrize("xt,yt", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
+def test_many_tokens(grad, M, N, K, xt, yt):
     """Tiles of pairs of CTAs: several to a pair, odd ones at every edge."""
-    check_linear(grad, M, *((K, N) if grad else (N, K)), "bf16", yt, pad=0 if K % 8 == 0 and N % 8 == 0 else 4)
-    check_linear(grad, M, *((K, N) if grad else (N, K)), "bf16", yt, pad=8, out_pad=3)
+    check_linear(grad, M, *((K, N) if grad else (N, K)), xt, yt)
+    check_linear(grad, M, *((K, N) if grad else (N, K)), xt, yt, pad=5, offset=1, out_pad=3)
 
 
 @pytest.mark.parametrize("grad", [False, True])
@@ -177,8 +177,9 @@ def test_not_a_number_stays_in_its_row_or_column(which):
     else:
         x[7, 11] = float("nan")
         x[9, 12] = float("inf")
-        y = pac.mxfp_linear(x, codes, scales)
-        assert y[7].isnan().all() and not y[9].isfinite().any() and y[[i for i in range(20) if i not in (7, 9)]].isfinite().all()
+        for x_ in (x, x.float()):
+            got, want = host(pac.mxfp_linear(x_, codes, scales)), (host(x)[:, None, :] * w[None]).sum(2)
+            assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want)) and np.isinf(want).any()
         y = pac.mxfp_product(*pac.quantize_mxfp(x), codes, scales, 200)
         assert y[[7, 9]].isnan().all() and y[:7].isfinite().all() and y[10:].isfinite().all()
 
@@ -205,24 +206,6 @@ def test_few_tokens_with_values_that_are_not_finite_and_of_all_sizes(xt):
     assert np.array_equal(got[[0, 1, 3, 4, 5, 6, 8]], host(y)[[0, 1, 3, 4, 5, 6, 8]])
 
 
-def test_few_tokens_without_a_workspace_and_with_one_too_small():
-    import paper_2408_10746_b200 as pac
-    lib = pac.load_library()
-    codes, scales, w = matrix(130, 200, 2)
-    x, y = torch.randn(3, 200, device="cuda"), torch.empty(3, 130, device="cuda")
-    n = lib.pac_mxfp_linear_workspace(3, 200)
-    assert n > 0 and lib.pac_mxfp_linear_workspace(17, 200) == 0
-    space = torch.empty(n, dtype=torch.uint8, device="cuda")
-    call = lambda at, size: lib.pac_mxfp_linear(0, torch.cuda.current_stream().cuda_stream, x.data_ptr(), 0, 3, 200, codes.data_ptr(), scales.data_ptr(), 130, 200,  # noqa: E731
-                                                y.data_ptr(), 0, 130, at, size)
-    assert call(space.data_ptr(), n - 1) == 1 and call(space.data_ptr() + 16, n) == 1
-    ref, size = host(x) @ w.T, np.abs(host(x)) @ np.abs(w.T)
-    for at, have in ((None, 0), (space.data_ptr(), n)):
-        y.fill_(float("nan"))
-        assert call(at, have) == 0
-        assert (np.abs(host(y) - ref) <= bound(ref, size, 200 / 16 + 16, torch.float32)).all()
-
-
 def test_filling_bytes_of_the_scales_do_not_matter_to_linear():
     import paper_2408_10746_b200 as pac
     codes, scales, w = matrix(100, 72, 4)
@@ -242,6 +225,19 @@ def test_filling_bytes_of_the_scales_do_not_matter_to_linear():
     got = pac.mxfp_linear(more, codes, scales)
     scales[0, 1] = 0
     assert torch.equal(pac.mxfp_linear(more, codes, scales), got) and got.isfinite().all()
+
+
+@pytest.mark.parametrize("M", [1, 20])
+def test_largest_fp32_values(M):
+    """The largest fp32 is beyond the largest bf16: its terms are finite all the same."""
+    import paper_2408_10746_b200 as pac
+    codes = np.full((128, 64), 1, np.uint8)                      # 0.5 everywhere, scale 1
+    packed, tiled = lo.pack(codes, np.full((128, 2), 127, np.uint8))
+    x = torch.zeros(M, 64, device="cuda")
+    x[0, 3], x[M - 1, 40] = torch.finfo(torch.float32).max, -torch.finfo(torch.float32).max
+    y = pac.mxfp_linear(x, torch.from_numpy(packed).cuda(), torch.from_numpy(tiled).cuda())
+    want = host(x).sum(1) / 2
+    assert (np.abs(host(y) - want[:, None]) <= 2.0 ** -22 * 2 * np.abs(host(x)).max() / 2).all()
 
 
 @pytest.mark.parametrize("s", [0, 1, 60, 200, 240])
