@@ -16,7 +16,8 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libpac_b200.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("pac_api.cu", "pac_lowbit_api.cu")]
 HEADERS = [os.path.join(HERE, "csrc", f) for f in ("pac_common.cuh", "pac_simt.cuh", "pac_tensor.cuh", "pac_mid.cuh", "pac_fused_fwd.cuh", "pac_gemm.cuh", "pac_quant.cuh", "pac_chain_fwd.cuh", "pac_tbody.cuh", "pac_xgemm.cuh", "pac_tbody_fused.cuh",
-                                                   "pac_ptx.cuh", "pac_adamw.cuh", "pac_adamw_tensors.cuh", "pac_mxfp.cuh", "pac_mxfp_linear.cuh", "pac_mxfp_pair.cuh", "pac_mxfp_product.cuh")] + \
+                                                   "pac_ptx.cuh", "pac_adamw.cuh", "pac_adamw_tensors.cuh", "pac_mxfp.cuh", "pac_mxfp_linear.cuh", "pac_mxfp_pair.cuh", "pac_mxfp_product.cuh",
+                                                   "pac_mxfp_product_pair.cuh")] + \
           [os.path.join(ROOT, "include", "pac.h")]
 
 

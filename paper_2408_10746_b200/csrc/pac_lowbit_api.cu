@@ -9,6 +9,7 @@
 #include "pac_mxfp_linear.cuh"
 #include "pac_mxfp_pair.cuh"
 #include "pac_mxfp_product.cuh"
+#include "pac_mxfp_product_pair.cuh"
 
 using namespace pac;
 
@@ -119,6 +120,41 @@ cudaError_t launch_product(int device, cudaStream_t st, const unsigned char* a_c
     cfg.attrs = attr;
     cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, mxfp_product_kernel, ma, mb, p);
+}
+
+// Scales as [row tiles][pieces][128] words, boxes of the two pieces of a K step.
+bool map_scales(CUtensorMap* map, const unsigned char* scales, long long rows, int K) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t pieces = (cuuint64_t)mx_col_pieces(K), dims[3] = {128, pieces, (cuuint64_t)((rows + 127) / 128)}, strides[2] = {512, 512 * pieces};
+    const cuuint32_t box[3] = {128, 2, 1}, ones[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<unsigned char*>(scales), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The same for many tokens, by pairs of CTAs.
+cudaError_t launch_product_pair(int device, cudaStream_t st, const unsigned char* a_codes, const unsigned char* a_scales, const unsigned char* b_codes,
+                                const unsigned char* b_scales, int K, const MqParams& p, int sms) {
+    CUtensorMap mx, mw, mxs, mws;
+    const long long row = mx_row_bytes(K);
+    if (!map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT8, a_codes, row, p.M, row, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !map_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, b_codes, row, p.cols, row, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !map_scales(&mxs, a_scales, p.M, K) || !map_scales(&mws, b_scales, p.cols, K))
+        return cudaErrorInvalidValue;
+    static OptedIn done;
+    const cudaError_t e = opt_in(done, (const void*)mxfp_product_pair_kernel, device);
+    if (e != cudaSuccess) return e;
+    const long long units = (long long)p.w_units * p.t_units;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2u * (unsigned)(units < sms / 2 ? units : sms / 2));
+    cfg.blockDim = dim3(MQ_THREADS);
+    cfg.dynamicSmemBytes = MQ_SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, mxfp_product_pair_kernel, mx, mw, mxs, mws, p);
 }
 
 // A few tokens as sums of matrices in MXFP4 (split_mxfp_kernel), then one block-scaled product.
@@ -286,13 +322,28 @@ extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsi
     if (!matrix_ok(dev_a_codes, dev_a_scales, M, K) || !dev_y || !aligned(dev_y, dtype_size(y_dtype)) || ldy < N) return PAC_ERR_INVALID_ARG;
     OnDevice on(device);
     if (!on.ok) return PAC_ERR_CUDA;
+    const int sms = sm_count(device);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e;
+    const long long units = (N + 255LL) / 256 * ((M + 255LL) / 256);
+    // pairs where their tiles fill more than half of the SMs; fp32 results up to 128 additions into an accumulator
+    if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (y_dtype != PAC_F32 || K <= 8192)) {
+        MqParams q = {};
+        q.y = dev_y; q.ldy = ldy; q.y_f32 = y_dtype == PAC_F32; q.M = M; q.cols = N; q.steps = (int)((K + 255LL) / 256);
+        q.w_units = (int)((N + 255LL) / 256); q.t_units = (int)((M + 255LL) / 256);
+        e = launch_product_pair(device, st, dev_a_codes, dev_a_scales, dev_b_codes, dev_b_scales, K, q, sms);
+        if (e == cudaSuccess) return PAC_OK;
+        cudaGetLastError();
+        return PAC_ERR_CUDA;
+    }
     MpParams p = {};
     p.a_scales = dev_a_scales; p.b_scales = dev_b_scales;
     p.o.y = dev_y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32; p.o.M = M; p.o.cols = N;
     p.pieces = mx_col_pieces(K);
     p.o.terms = 1;
-    if (!mp_plan(p, K, sm_count(device))) return PAC_ERR_UNSUPPORTED;
-    if (launch_product(device, (cudaStream_t)cuda_stream, dev_a_codes, M, dev_b_codes, K, p) == cudaSuccess) return PAC_OK;
+    if (!mp_plan(p, K, sms)) return PAC_ERR_UNSUPPORTED;
+    e = launch_product(device, st, dev_a_codes, M, dev_b_codes, K, p);
+    if (e == cudaSuccess) return PAC_OK;
     cudaGetLastError();
     return PAC_ERR_CUDA;
 }

@@ -46,8 +46,8 @@ __device__ __forceinline__ uint64_t smem_desc_plain(uint32_t saddr) {
 }
 // Instruction descriptor, kind::mxf4: A and B E2M1 (bits 7, 10), both K-major, N >> 3 at bit 17, scales UE8M0 (bit 23), M >> 7 at
 // bit 27; which half of a word of scales this K step uses (0 or 2): bits 4 (B) and 29 (A).
-__device__ __forceinline__ uint32_t instr_desc_mxf4(int N, uint32_t half) {
-    return (half << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | (1u << 27) | (half << 29);
+__device__ __forceinline__ uint32_t instr_desc_mxf4(int M, int N, uint32_t half) {
+    return (half << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27) | (half << 29);
 }
 
 // A block of x with an infinity or a NaN has no terms but a scale that is not a number, so every sum that it enters comes out
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(320, 2) mxfp_product_kernel(const __grid_const
             if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
         }
     } else if (warp == 1) {
-        const uint32_t idesc0 = instr_desc_mxf4(p.o.nt, 0u), idesc1 = instr_desc_mxf4(p.o.nt, 2u);
+        const uint32_t idesc0 = instr_desc_mxf4(128, p.o.nt, 0u), idesc1 = instr_desc_mxf4(128, p.o.nt, 2u);
         const uint64_t w0 = smem_desc_sw128(ring0, 16, 1024), x0 = smem_desc_sw128(ring0 + MP_W_BYTES, 16, 1024), f0 = smem_desc_plain(ring0 + sf_at);
         uint32_t s = 0, ph = 0, acc = 0;
         for (int i = 0; i < k1 - k0; ++i) {

@@ -255,7 +255,7 @@ def test_extreme_scales_are_exact(s):
 
 # ---------------------------------------------------------------- both operands in 4 bits
 @pytest.mark.parametrize("yt", ["bf16", "f32"])
-@pytest.mark.parametrize("M,N,K", SHAPES + [(513, 130, 300), (1, 64, 257)])
+@pytest.mark.parametrize("M,N,K", SHAPES + [(513, 130, 300), (1, 64, 257), (1000, 3000, 136), (520, 8200, 300), (2049, 1300, 520), (700, 2600, 1280)])
 def test_product_of_two_matrices_in_four_bits(M, N, K, yt):
     import paper_2408_10746_b200 as pac
     a, b = matrix(M, K, M + 1), matrix(N, K, N + 2)
@@ -265,10 +265,11 @@ def test_product_of_two_matrices_in_four_bits(M, N, K, yt):
     assert (off <= bound(ref, size, K / 64 + 16, TYPES[yt])).all(), (off / size).max()
 
 
-def test_every_scale_and_every_pair_of_codes_in_the_block_scaled_product():
+@pytest.mark.parametrize("n", [256, 5000])
+def test_every_scale_and_every_pair_of_codes_in_the_block_scaled_product(n):
     """Row i of A has code i % 16 in column i and 0 elsewhere, so y[i][j] is one product: all pairs, all positions, all scales."""
     import paper_2408_10746_b200 as pac
-    K, N = 512, 256
+    K, N = 512, n
     codes = np.zeros((K, K), np.uint8)
     codes[np.arange(K), np.arange(K)] = np.arange(K) % 16
     rng = np.random.default_rng(0)
