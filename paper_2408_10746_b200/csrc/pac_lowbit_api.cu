@@ -276,8 +276,9 @@ extern "C" pac_status pac_quantize_mxfp(int device, void* cuda_stream, const voi
     const long long want = (items + 7) / 8, most = 148LL * 32;
     const unsigned grid = (unsigned)(want < most ? want : most);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == PAC_F32) quantize_mxfp_kernel<float><<<grid, 256, 0, st>>>((const float*)dev_x, rows, cols, ldx, vec, dev_codes, dev_scales);
-    else quantize_mxfp_kernel<bf16><<<grid, 256, 0, st>>>((const bf16*)dev_x, rows, cols, ldx, vec, dev_codes, dev_scales);
+    const MxDiv by_pairs(mx_col_pieces(cols) / 2, items);
+    if (dtype == PAC_F32) quantize_mxfp_kernel<float><<<grid, 256, 0, st>>>((const float*)dev_x, rows, cols, ldx, vec, dev_codes, dev_scales, by_pairs);
+    else quantize_mxfp_kernel<bf16><<<grid, 256, 0, st>>>((const bf16*)dev_x, rows, cols, ldx, vec, dev_codes, dev_scales, by_pairs);
     return launched();
 }
 
@@ -289,11 +290,18 @@ extern "C" pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const u
     OnDevice on(device);
     if (!on.ok) return PAC_ERR_CUDA;
     const bool vec = aligned(dev_out, 32) && (ldo * (long long)dtype_size(dtype)) % 32 == 0;
-    const long long want = (rows * (mx_row_bytes(cols) / 8) + 255) / 256, most = 148LL * 32;
+    const long long per_row = mx_row_bytes(cols) / (vec ? 8 : 1), items = rows * per_row;
+    const long long want = (items + 255) / 256, most = 148LL * 32;
     const unsigned grid = (unsigned)(want < most ? want : most);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == PAC_F32) dequantize_mxfp_kernel<float><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (float*)dev_out, ldo, vec);
-    else dequantize_mxfp_kernel<bf16><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (bf16*)dev_out, ldo, vec);
+    const MxDiv by_row(per_row, items);
+    if (vec) {
+        if (dtype == PAC_F32) dequantize_mxfp_kernel<float><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (float*)dev_out, ldo, by_row);
+        else dequantize_mxfp_kernel<bf16><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (bf16*)dev_out, ldo, by_row);
+    } else {
+        if (dtype == PAC_F32) dequantize_mxfp_any_kernel<float><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (float*)dev_out, ldo, by_row);
+        else dequantize_mxfp_any_kernel<bf16><<<grid, 256, 0, st>>>(dev_codes, dev_scales, rows, cols, (bf16*)dev_out, ldo, by_row);
+    }
     return launched();
 }
 

@@ -21,14 +21,19 @@ __host__ __device__ inline int mx_col_pieces(int cols) { return 2 * (int)(((long
 // Byte of a scale within its 512-byte piece; r = row % 128, b = block of the piece.
 __host__ __device__ inline uint32_t mx_scale_at(uint32_t r, uint32_t b) { return (r & 31u) * 16u + (r >> 5) * 4u + b; }
 
-// Sixteen codes of sixteen values times a power of two.
+// Eight codes of eight values times a power of two.
 __device__ __forceinline__ uint32_t mx_codes8(const float* v, float f) {
+    float a[8];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)                           // two products in one instruction
+        asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %4};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+            : "=f"(a[e]), "=f"(a[e + 1]) : "f"(v[e]), "f"(v[e + 1]), "f"(f));
     uint32_t w;
     asm("{\n .reg .b8 b0, b1, b2, b3;\n"
         " cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
         " cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
         " mov.b32 %0, {b0, b1, b2, b3};\n}"
-        : "=r"(w) : "f"(v[0] * f), "f"(v[1] * f), "f"(v[2] * f), "f"(v[3] * f), "f"(v[4] * f), "f"(v[5] * f), "f"(v[6] * f), "f"(v[7] * f));
+        : "=r"(w) : "f"(a[0]), "f"(a[1]), "f"(a[2]), "f"(a[3]), "f"(a[4]), "f"(a[5]), "f"(a[6]), "f"(a[7]));
     return w;
 }
 // Eight codes -> four pairs of bf16 in the order of the columns, before the scale: both bytes of |value| from a table by
@@ -55,67 +60,99 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     return d;
 }
 
-// Sixteen consecutive values; `vec`: 32-byte accesses are allowed and all sixteen exist.  `have` of them exist otherwise.
-__device__ __forceinline__ void mx_load16(const float* p, bool vec, int have, float (&v)[16]) {
-    if (vec) {
+// Sixteen consecutive values as they lie in memory; `vec`: 32-byte accesses are allowed and all sixteen exist, else `have` of
+// them do.  top(): the bits of the largest magnitude as fp32 (they order infinities and NaN above everything else).
+template <typename T> struct MxRaw;
+template <> struct MxRaw<float> {
+    float v[16];
+    __device__ __forceinline__ void load(const float* p, bool vec, int have) {
+        if (vec && have >= 16) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            asm volatile("ld.global.nc.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                         : "=f"(v[8 * h]), "=f"(v[8 * h + 1]), "=f"(v[8 * h + 2]), "=f"(v[8 * h + 3]), "=f"(v[8 * h + 4]), "=f"(v[8 * h + 5]),
-                           "=f"(v[8 * h + 6]), "=f"(v[8 * h + 7]) : "l"(p + 8 * h));
-    } else {
+            for (int h = 0; h < 2; ++h)
+                asm volatile("ld.global.nc.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=f"(v[8 * h]), "=f"(v[8 * h + 1]), "=f"(v[8 * h + 2]), "=f"(v[8 * h + 3]), "=f"(v[8 * h + 4]), "=f"(v[8 * h + 5]),
+                               "=f"(v[8 * h + 6]), "=f"(v[8 * h + 7]) : "l"(p + 8 * h));
+        } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = e < have ? p[e] : 0.f;
-    }
-}
-__device__ __forceinline__ void mx_load16(const bf16* p, bool vec, int have, float (&v)[16]) {
-    if (vec) {
-        uint32_t u[8];
-        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]) : "l"(p));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[2 * e] = __uint_as_float(u[e] << 16);
-            v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+            for (int e = 0; e < 16; ++e) v[e] = e < have ? p[e] : 0.f;
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = e < have ? __bfloat162float(p[e]) : 0.f;
     }
-}
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t t = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t = max(t, __float_as_uint(v[e]) & 0x7fffffffu);
+        return t;
+    }
+    __device__ __forceinline__ void values(float (&x)[16]) const {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = v[e];
+    }
+};
+template <> struct MxRaw<bf16> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const bf16* p, bool vec, int have) {
+        if (vec && have >= 16) {
+            asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                w[e] = (2 * e < have ? (uint32_t)__bfloat16_as_ushort(p[2 * e]) : 0u) | (2 * e + 1 < have ? (uint32_t)__bfloat16_as_ushort(p[2 * e + 1]) << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t t = 0;                                      // both halves at once
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t = __vmaxu2(t, w[e] & 0x7fff7fffu);
+        return max(t << 16, t & 0xffff0000u);
+    }
+    __device__ __forceinline__ void values(float (&x)[16]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { x[2 * e] = __uint_as_float(w[e] << 16); x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
+    }
+};
+
+// n / d for d >= 1: a multiplication by m = ceil(2^(31 + s) / d), 2^s >= d > 2^(s-1), where n < 2^31 (m < 2^32, and what m is too
+// large by adds less than n / 2^31 / d to the quotient); a 64-bit division otherwise.  (The codec spent a third of its
+// instructions on the latter.)
+struct MxDiv {
+    long long d;
+    uint32_t m, s;                                          // m == 0: d is 1
+    bool small;
+    MxDiv(long long d_, long long most) : d(d_), m(0), s(1), small(most < (1LL << 31) && d_ < (1LL << 31)) {
+        while ((1LL << s) < d) ++s;
+        if (small && d > 1) m = (uint32_t)(((1ULL << (31 + s)) + (unsigned long long)d - 1) / (unsigned long long)d);
+    }
+    __device__ __forceinline__ long long div(long long n) const {
+        if (!small) return n / d;
+        return m ? (long long)(__umulhi((uint32_t)n, m) >> (s - 1)) : n;
+    }
+};
 
 // A warp takes four rows and 256 columns (two pieces of scales) at a time: eight lanes to a row, sixteen values to a lane
 // and piece, two lanes to a block.  The rows and pieces that only fill up a tile are walked too: their scales are written
 // as 0, so that a product may read whole pieces.  Bound by HBM (4.53 or 2.53 bytes per value).
 template <typename T>
 __global__ void __launch_bounds__(256) quantize_mxfp_kernel(const T* __restrict__ x, long long rows, int cols, long long ldx, bool vec,
-                                                            unsigned char* __restrict__ codes, unsigned char* __restrict__ scales) {
+                                                            unsigned char* __restrict__ codes, unsigned char* __restrict__ scales, const MxDiv by_pairs) {
     const int lane = threadIdx.x & 31, in_row = lane & 7;
     const int pieces = mx_col_pieces(cols);
     const long long row_bytes = mx_row_bytes(cols);
     const long long groups = (rows + MX_TILE - 1) / MX_TILE * (MX_TILE / 4), items = groups * (pieces / 2);
     const long long warps = ((long long)gridDim.x * blockDim.x) >> 5;
     for (long long it = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5; it < items; it += warps) {
-        const long long g = it / (pieces / 2);
+        const long long g = by_pairs.div(it);
         const int cp = 2 * (int)(it - g * (pieces / 2));
         const long long row = g * 4 + (lane >> 3);
-        float v[2][16];
+        MxRaw<T> raw[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int c0 = (cp + h) * MX_TILE + in_row * 16;
-            const int have = row < rows ? cols - c0 : 0;
-            if (have > 0) mx_load16(x + row * ldx + c0, vec && have >= 16, have, v[h]);
-            else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[h][e] = 0.f;
-            }
+            raw[h].load(x + row * ldx + c0, vec, row < rows ? cols - c0 : 0);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            // the largest magnitude as bits: orders infinities and NaN above everything else
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(v[h][e]) & 0x7fffffffu);
+            uint32_t top = raw[h].top();
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             const uint32_t ex = top >> 23;
             const bool finite = ex < 255u;
@@ -124,7 +161,9 @@ __global__ void __launch_bounds__(256) quantize_mxfp_kernel(const T* __restrict_
             const int c0 = (cp + h) * MX_TILE + in_row * 16;
             if (row < rows && (c0 & ~31) < cols) {
                 uint2 w = make_uint2(0u, 0u);
-                if (finite) w = make_uint2(mx_codes8(&v[h][0], f), mx_codes8(&v[h][8], f));
+                float v[16];
+                raw[h].values(v);
+                if (finite) w = make_uint2(mx_codes8(v, f), mx_codes8(v + 8, f));
                 *reinterpret_cast<uint2*>(codes + row * row_bytes + (c0 >> 1)) = w;
             }
             // the four scales of a row and piece as one word
@@ -139,49 +178,77 @@ __global__ void __launch_bounds__(256) quantize_mxfp_kernel(const T* __restrict_
     }
 }
 
-// Sixteen values to a lane, as above.  Bound by HBM.
+// Sixteen values to a lane, as above; rows begin on 32-byte boundaries.  Bound by HBM.
 template <typename T>
 __global__ void __launch_bounds__(256) dequantize_mxfp_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
-                                                              long long rows, int cols, T* __restrict__ out, long long ldo, bool vec) {
+                                                              long long rows, int cols, T* __restrict__ out, long long ldo, const MxDiv by_row) {
     const int pieces = mx_col_pieces(cols);
     const long long row_bytes = mx_row_bytes(cols);
     const long long per_row = row_bytes >> 3, items = rows * per_row;
     for (long long it = (long long)blockIdx.x * blockDim.x + threadIdx.x; it < items; it += (long long)gridDim.x * blockDim.x) {
-        const long long row = it / per_row;
+        const long long row = by_row.div(it);
         const int at = (int)(it - row * per_row), c0 = at * 16;
         const uint2 w = *reinterpret_cast<const uint2*>(codes + it * 8);
         const uint32_t s = scales[((row / MX_TILE) * pieces + c0 / MX_TILE) * (long long)MX_SCALE_PIECE + mx_scale_at((uint32_t)(row % MX_TILE), (uint32_t)(c0 % MX_TILE) / MX_BLOCK)];
         uint32_t o[2][4];
         mx_bf16x8(w.x, o[0]);
         mx_bf16x8(w.y, o[1]);
-        const float f = mx_scale_f32(s);
-        float v[16];
+        if constexpr (sizeof(T) == 2) {                      // a value times its power of two is a bf16 exactly
+            const uint32_t f = mx_scale_bf16x2(s);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[2 * e] = __uint_as_float(o[e >> 2][e & 3] << 16) * f;
-            v[2 * e + 1] = __uint_as_float(o[e >> 2][e & 3] & 0xffff0000u) * f;
+            for (int e = 0; e < 8; ++e) o[e >> 2][e & 3] = mul_bf16x2(o[e >> 2][e & 3], f);
+        }
+        float v[16];
+        if constexpr (sizeof(T) == 4) {
+            const float f = mx_scale_f32(s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[2 * e] = __uint_as_float(o[e >> 2][e & 3] << 16) * f;
+                v[2 * e + 1] = __uint_as_float(o[e >> 2][e & 3] & 0xffff0000u) * f;
+            }
         }
         T* dst = out + row * ldo + c0;
-        if (vec && c0 + 16 <= cols) {
+        if (c0 + 16 <= cols) {
             if constexpr (sizeof(T) == 4) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     st_global_32(dst + 8 * h, make_uint4(__float_as_uint(v[8 * h]), __float_as_uint(v[8 * h + 1]), __float_as_uint(v[8 * h + 2]), __float_as_uint(v[8 * h + 3])),
                                  make_uint4(__float_as_uint(v[8 * h + 4]), __float_as_uint(v[8 * h + 5]), __float_as_uint(v[8 * h + 6]), __float_as_uint(v[8 * h + 7])));
             } else {
-                uint32_t u[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = bf16_pair(v[2 * e], v[2 * e + 1]);
-                st_global_32(dst, make_uint4(u[0], u[1], u[2], u[3]), make_uint4(u[4], u[5], u[6], u[7]));
+                st_global_32(dst, make_uint4(o[0][0], o[0][1], o[0][2], o[0][3]), make_uint4(o[1][0], o[1][1], o[1][2], o[1][3]));
             }
         } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 if (c0 + e < cols) {
                     if constexpr (sizeof(T) == 4) dst[e] = v[e];
-                    else dst[e] = __float2bfloat16(v[e]);
+                    else dst[e] = __ushort_as_bfloat16((unsigned short)(o[e >> 3][(e >> 1) & 3] >> (16 * (e & 1))));
                 }
         }
+    }
+}
+// Rows that do not begin on 32-byte boundaries: two values to a lane, so that a warp's stores are neighbours (sixteen to a lane
+// and element by element, 8192 x 770 took 38 us).
+template <typename T>
+__global__ void __launch_bounds__(256) dequantize_mxfp_any_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
+                                                                  long long rows, int cols, T* __restrict__ out, long long ldo, const MxDiv by_row) {
+    const int pieces = mx_col_pieces(cols);
+    const long long row_bytes = mx_row_bytes(cols), items = rows * row_bytes;
+    for (long long it = (long long)blockIdx.x * blockDim.x + threadIdx.x; it < items; it += (long long)gridDim.x * blockDim.x) {
+        const long long row = by_row.div(it);
+        const int c0 = 2 * (int)(it - row * row_bytes);
+        const uint32_t w = codes[it];
+        const float f = mx_scale_f32(scales[((row / MX_TILE) * pieces + c0 / MX_TILE) * (long long)MX_SCALE_PIECE + mx_scale_at((uint32_t)(row % MX_TILE), (uint32_t)(c0 % MX_TILE) / MX_BLOCK)]);
+        uint32_t o[4];
+        mx_bf16x8(w, o);
+        T* dst = out + row * ldo + c0;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (c0 + e < cols) {
+                const float v = __uint_as_float(e ? o[0] & 0xffff0000u : o[0] << 16) * f;
+                if constexpr (sizeof(T) == 4) dst[e] = v;
+                else dst[e] = __float2bfloat16(v);
+            }
     }
 }
 
