@@ -72,6 +72,22 @@ cudaError_t opt_in(OptedIn& done, const void* kernel, int device) {
     return e;
 }
 
+// Attributes of a launch in clusters of `split`; `after`: it may begin while the kernel before it runs (and waits for it).
+unsigned launch_attributes(cudaLaunchAttribute* attr, int split, bool after) {
+    unsigned n = 0;
+    if (split > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)split; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (after) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    return n;
+}
+
 template <bool GRAD, int TERMS>
 cudaError_t launch_linear(int device, cudaStream_t st, const CUtensorMap& codes, const CUtensorMap& x, const MlParams& p) {
     const auto kernel = mxfp_linear_kernel<GRAD, TERMS>;
@@ -83,11 +99,9 @@ cudaError_t launch_linear(int device, cudaStream_t st, const CUtensorMap& codes,
     cfg.blockDim = dim3(32 * (2 + ML_CONV_WARPS));
     cfg.dynamicSmemBytes = 1024 + p.code_at + (size_t)p.code_stages * ML_CODE_BYTES;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.o.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
     cfg.attrs = attr;
-    cfg.numAttrs = p.o.split > 1 ? 1 : 0;
+    cfg.numAttrs = launch_attributes(attr, p.o.split, p.after);
     return cudaLaunchKernelEx(&cfg, kernel, codes, x, p);
 }
 
@@ -106,19 +120,8 @@ cudaError_t launch_product(int device, cudaStream_t st, const unsigned char* a_c
     cfg.dynamicSmemBytes = mp_smem(p);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    unsigned n = 0;
-    if (p.o.split > 1) {
-        attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = (unsigned)p.o.split; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
-        ++n;
-    }
-    if (p.after) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n].val.programmaticStreamSerializationAllowed = 1;
-        ++n;
-    }
     cfg.attrs = attr;
-    cfg.numAttrs = n;
+    cfg.numAttrs = launch_attributes(attr, p.o.split, p.after);
     return cudaLaunchKernelEx(&cfg, mxfp_product_kernel, ma, mb, p);
 }
 
@@ -256,6 +259,7 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     p.o.terms = 1;
     p.scales = scales; p.o.y = y; p.o.ldy = ldy; p.o.y_f32 = y_f32;
     p.o.M = M; p.o.cols = out_cols; p.red = red; p.pieces = mx_col_pieces(K); p.x_rows = M;
+    p.after = need > 0;
     if (!ml_plan(p, terms == 3, sms)) return PAC_ERR_UNSUPPORTED;
     if (!map_x(p.o.nt)) return PAC_ERR_CUDA;
     if (grad) return status(terms == 3 ? launch_linear<true, 3>(device, st, mc, mx, p) : launch_linear<true, 1>(device, st, mc, mx, p));

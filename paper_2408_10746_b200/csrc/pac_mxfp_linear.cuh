@@ -53,6 +53,7 @@ struct MlParams {
     uint32_t stage_bytes, code_at;                          // bytes per stage; offset of the ring of codes
     uint32_t tmem_cols;
     int x_rows;                                             // rows of a term of x
+    bool after;                                             // launched ahead of the end of the kernel that packs x
 };
 
 __device__ __forceinline__ void ml_tma_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
@@ -189,6 +190,7 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
 __host__ __device__ inline int pack_columns(int red) { return (red + 127) / 128 * 128; }
 template <typename T>
 __global__ void __launch_bounds__(256) pack_tokens_kernel(const T* __restrict__ x, int M, int red, long long ldx, bool vec, bf16* __restrict__ out) {
+    pdl_trigger();
     const int cols = pack_columns(red), groups = cols / 8;
     const long long items = (long long)M * groups, term = (long long)M * cols;
     for (long long it = (long long)blockIdx.x * blockDim.x + threadIdx.x; it < items; it += (long long)gridDim.x * blockDim.x) {
@@ -332,6 +334,7 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
                 ok = mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr);
                 if (!ok) break;
                 if (elect_one()) {
+                    if (p.after && kt == kt0 && h == 0) pdl_wait();
                     mbar_expect_tx(xfull0 + 8 * s, TERMS * term_bytes);
 #pragma unroll
                     for (int e = 0; e < TERMS; ++e)          // (rows of a tile past the last token may be another term's: no one stores them)
@@ -413,13 +416,13 @@ inline bool ml_plan(MlParams& p, bool f32_terms, int sms) {
     p.o.n_acc = f32_terms ? 5 : (512 / p.o.nt < 4 ? 512 / p.o.nt : 4);
     p.tmem_cols = 32;
     while (p.tmem_cols < (uint32_t)(p.o.n_acc * p.o.nt)) p.tmem_cols *= 2;
-    // as many CTAs as there are SMs, at least two pieces each; fp32 results: at most 128 additions into an accumulator
+    // as many CTAs as there are SMs; fp32 results: at most 128 additions into an accumulator
     p.o.split = 1;
     const long long ctas = (long long)wts * tok_tiles;
-    while (p.o.split < 8 && p.o.split * 4 <= p.red_tiles && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
+    while (p.o.split < 8 && p.o.split * 2 <= p.red_tiles && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
     if (p.o.y_f32) {
         const int lead = f32_terms ? p.o.n_acc - 1 : p.o.n_acc;
-        while (p.o.split < 8 && p.o.split * 4 <= p.red_tiles && (long long)p.red_tiles * 8 > 128LL * lead * p.o.split) p.o.split *= 2;
+        while (p.o.split < 8 && p.o.split * 2 <= p.red_tiles && (long long)p.red_tiles * 8 > 128LL * lead * p.o.split) p.o.split *= 2;
     }
     p.stage_bytes = ML_A_BYTES + (uint32_t)p.o.nt * 128u * (f32_terms ? 3u : 1u);
     p.code_stages = p.o.nt > 128 ? 3 : 6;
