@@ -182,7 +182,13 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
             else static_cast<bf16*>(o.y)[at] = __float2bfloat16(y);
         }
     }
-    if (o.split > 1) cluster.sync();                         // nobody leaves while its partial sums are still read
+    // nobody leaves while its partial sums are still read (they have been: what is added up is in registers); the stores of y need
+    // no ordering here, and waiting for them cost 1500 clocks
+    if (o.split > 1) {
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
 }
 
 // x as TMA boxes can read it: TERMS matrices [rows][16-byte rows of whole 128-column pieces] in bf16, below one another.  A bf16 x
