@@ -128,7 +128,7 @@ def load_library() -> C.CDLL:
     lib.pac_adamw_tensors.argtypes = [I, P, C.POINTER(_AdamWTensor), I, I, C.POINTER(_AdamW), LL, P, F, C.c_uint]
     for name in ("pac_quantize_mxfp", "pac_dequantize_mxfp", "pac_mxfp_linear", "pac_mxfp_linear_grad", "pac_mxfp_product", "pac_adamw_tensors"):
         getattr(lib, name).restype = I
-    lib.pac_mxfp_linear_workspace.argtypes = [P, I, I, LL, I, I]
+    lib.pac_mxfp_linear_workspace.argtypes = [P, I, I, LL, I, I, I]
     lib.pac_mxfp_linear_workspace.restype = LL
     lib.pac_last_error.argtypes = [P]
     lib.pac_last_error.restype = C.c_char_p
@@ -608,7 +608,7 @@ def _mxfp_linear(call, lib, x, M: int, ld: int, codes, scales, N: int, K: int, g
     dtype = dtype or (out.dtype if out is not None else x.dtype)
     device, xt, yt, at = x.device, _dtype(x.dtype), _dtype(dtype), x.data_ptr()
     out, ldo = _out(out, M, K if grad else N, dtype, device)
-    n = lib.pac_mxfp_linear_workspace(at, xt, M, ld, N if grad else K, grad)
+    n = lib.pac_mxfp_linear_workspace(at, xt, M, ld, N, K, grad)
     space = codes.new_empty(n) if n else None
     st = call(device.index, _stream(device.index), at, xt, M, ld, codes.data_ptr(), scales.data_ptr(), N, K, out.data_ptr(), yt, ldo,
               space.data_ptr() if n else None, n)

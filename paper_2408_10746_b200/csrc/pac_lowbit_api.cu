@@ -107,8 +107,8 @@ cudaError_t launch_linear(int device, cudaStream_t st, const CUtensorMap& codes,
 
 // y = A B^T on the block-scaled tensor cores; `rows` of A's codes.
 cudaError_t launch_product(int device, cudaStream_t st, const unsigned char* a_codes, int rows, const unsigned char* b_codes, int K, MpParams& p) {
-    CUtensorMap ma, mb;
-    if (!map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, a_codes, mx_row_bytes(K), rows, mx_row_bytes(K), 128, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B) ||
+    CUtensorMap ma = {}, mb;
+    if ((!p.here && !map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, a_codes, mx_row_bytes(K), rows, mx_row_bytes(K), 128, p.o.nt, CU_TENSOR_MAP_SWIZZLE_128B)) ||
         !map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, b_codes, mx_row_bytes(K), p.o.cols, mx_row_bytes(K), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
     static OptedIn done;
@@ -167,10 +167,12 @@ cudaError_t few_tokens(int device, cudaStream_t st, const void* x, int x_dtype, 
     MpParams p = {};
     p.a_scales = space + w.scales; p.b_scales = scales; p.b_codes = codes;
     p.x = x; p.ldx = ldx; p.x_f32 = x_dtype == PAC_F32; p.K = K;
-    p.after = true;
+    p.here = ms_here(M, N, K);
+    p.after = !p.here;
     p.o.y = y; p.o.ldy = ldy; p.o.y_f32 = y_dtype == PAC_F32; p.o.M = M; p.o.cols = N; p.o.terms = MS_TERMS;
     p.pieces = mx_col_pieces(K);
     if (!mp_plan(p, K, sm_count(device))) return cudaErrorInvalidValue;
+    if (p.here) return launch_product(device, st, nullptr, M * MS_TERMS, codes, K, p);
     const unsigned grid = (unsigned)(((long long)M * p.pieces * 4 + 7) / 8);
     if (x_dtype == PAC_F32) split_mxfp_kernel<float><<<grid, 256, 0, st>>>((const float*)x, M, K, ldx, space + w.codes, space + w.scales);
     else split_mxfp_kernel<bf16><<<grid, 256, 0, st>>>((const bf16*)x, M, K, ldx, space + w.codes, space + w.scales);
@@ -202,8 +204,9 @@ cudaError_t launch_pair(int device, cudaStream_t st, const CUtensorMap& codes, c
 bool few(bool grad, int M) { return !grad && M <= MS_MOST_TOKENS; }
 // Rows that TMA boxes can read as they are.
 bool boxes(const void* x, int dtype, long long ldx) { return dtype == PAC_BF16 && aligned(x, 16) && ldx % 8 == 0; }
-long long linear_space(bool grad, const void* x, int dtype, int M, long long ldx, int red) {
-    if (few(grad, M)) return ms_space(M, red).bytes;
+long long linear_space(bool grad, const void* x, int dtype, int M, long long ldx, int N, int K) {
+    if (few(grad, M)) return ms_here(M, N, K) ? 0 : ms_space(M, K).bytes;
+    const int red = grad ? N : K;
     return boxes(x, dtype, ldx) ? 0 : (dtype == PAC_F32 ? 6LL : 2LL) * M * pack_columns(red);
 }
 
@@ -214,7 +217,7 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     if (M == 0) return PAC_OK;
     if (!x || !y || ldx < red || ldy < out_cols || M > 0x0fffff00) return PAC_ERR_INVALID_ARG;
     if (!aligned(x, dtype_size(x_dtype)) || !aligned(y, dtype_size(y_dtype))) return PAC_ERR_INVALID_ARG;
-    const long long need = linear_space(grad, x, x_dtype, M, ldx, red);
+    const long long need = linear_space(grad, x, x_dtype, M, ldx, N, K);
     if (need > 0 && (!space || !aligned(space, 256) || space_bytes < need)) return PAC_ERR_INVALID_ARG;
     OnDevice on(device);
     if (!on.ok) return PAC_ERR_CUDA;
@@ -315,9 +318,9 @@ extern "C" pac_status pac_mxfp_linear(int device, void* cuda_stream, const void*
     return mxfp_linear(false, device, cuda_stream, dev_x, x_dtype, M, ldx, dev_codes, dev_scales, N, K, dev_y, y_dtype, ldy, dev_workspace, workspace_bytes);
 }
 
-extern "C" long long pac_mxfp_linear_workspace(const void* dev_x, int x_dtype, int M, long long ldx, int reduction, int grad) {
-    if (M < 1 || M > 0x0fffff00 || reduction < 1 || reduction > 0x7fffff00 || !dtype_ok(x_dtype)) return 0;
-    return linear_space(grad != 0, dev_x, x_dtype, M, ldx, reduction);
+extern "C" long long pac_mxfp_linear_workspace(const void* dev_x, int x_dtype, int M, long long ldx, int N, int K, int grad) {
+    if (M < 1 || M > 0x0fffff00 || N < 1 || N > 0x7fffff00 || K < 1 || K > 0x7fffff00 || !dtype_ok(x_dtype)) return 0;
+    return linear_space(grad != 0, dev_x, x_dtype, M, ldx, N, K);
 }
 
 extern "C" pac_status pac_mxfp_linear_grad(int device, void* cuda_stream, const void* dev_dy, int dy_dtype, int M, long long lddy,

@@ -14,7 +14,7 @@ constexpr int MP_BK = 256, MP_MAX_STAGES = 8;
 constexpr uint32_t MP_W_BYTES = 128 * 128;
 constexpr uint32_t MP_SF_COLS = 24;                          // scales in tensor memory: two sets of up to 24 columns behind the accumulators
 // Tokens that are not in 4 bits, a few of them (pac_mxfp_linear): as sums of MS_TERMS matrices in MXFP4, see split_mxfp_kernel.
-constexpr int MS_TERMS = 12, MS_MOST_TOKENS = 16;
+constexpr int MS_TERMS = 12, MS_MOST_TOKENS = 16, MS_HERE = 4;
 
 struct MpParams {
     MxOut o;
@@ -25,6 +25,7 @@ struct MpParams {
     uint32_t x_bytes, stage_bytes;
     uint32_t tmem_cols, sf_col;
     bool after;                                             // launched ahead of the end of the kernel that writes A
+    bool here;                                              // one or two tokens: the terms of x are made in this kernel, step by step
     // sums of terms: what a result that is not a number is formed from again
     const void* x; long long ldx; int x_f32; int K;
     const unsigned char* b_codes;
@@ -50,6 +51,47 @@ __device__ __forceinline__ uint32_t instr_desc_mxf4(int M, int N, uint32_t half)
     return (half << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27) | (half << 29);
 }
 
+// A block of x, a value per lane, as a sum of MS_TERMS blocks in MXFP4: the first is x rounded, each next one is what the ones
+// before it leave, rounded with a scale two powers of two finer.  What a term leaves is at most 2 of its units (of [6, 8), which
+// become 6; else at most 1), so it is below 8 of the next one's, and the twelfth leaves at most 2^-23 of the largest of the 32
+// (mostly 2^-26): bf16 values within 2^14 of each other enter exactly.  With it the products of a few tokens are block-scaled
+// products of the codes of W as they are: nothing converts W, whose bytes are the floor.  (Scales from the remainders' own
+// largest gain 0.6 bits a term and cost a reduction over the warp in each of the twelve dependent rounds: twice the time.)
+// put_codes(term, word): the codes of this lane's eight neighbours (lane / 8); put_scale(term, byte).  Terms 8 .. 11 come with
+// lanes 0 .. 3 of the eight.
+template <typename PutCodes, typename PutScale>
+__device__ __forceinline__ void ms_terms(float r, PutCodes put_codes, PutScale put_scale) {
+    const uint32_t lane = threadIdx.x & 31;
+    const bool finite = !__any_sync(0xffffffffu, !(fabsf(r) < __uint_as_float(0x7f800000u)));
+    if (!finite) r = 0.f;
+    const int e0 = (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(r) & 0x7fffffffu) >> 23) - 2;
+    uint32_t w[2] = {0u, 0u};                                // term t's code: nibble t % 8 of word t / 8
+#pragma unroll
+    for (int t = 0; t < MS_TERMS; ++t) {
+        const uint32_t s = (uint32_t)max(e0 - 2 * t, 0);
+        uint32_t c;
+        asm("{\n .reg .b8 b0;\n cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n mov.b32 %0, {b0, b0, b0, b0};\n}"
+            : "=r"(c) : "f"(r * __uint_as_float((254u - s) << 23)), "f"(0.f));
+        c &= 15u;
+        const uint32_t mag = c & 7u;
+        const float v = __uint_as_float((mag < 2u ? mag * 0x3f000000u : (mag + 252u) << 22) | (c & 8u) << 28);
+        r = fmaf(v, -mx_scale_f32(s), r);                    // exact: both are multiples of r's last bit, and the difference is smaller
+        w[t >> 3] |= c << (4 * (t & 7));
+    }
+    // eight lanes x eight nibbles transposed: lane j of the eight gets the codes of term j
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (uint32_t d = 4; d >= 1; d >>= 1) {
+            const uint32_t low = d == 4 ? 0x0000ffffu : d == 2 ? 0x00ff00ffu : 0x0f0f0f0fu;
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, w[h], d);
+            w[h] = (lane & d) ? (w[h] & ~low) | ((other >> (4 * d)) & low) : (w[h] & low) | ((other & low) << (4 * d));
+        }
+    const int t = (int)(lane & 7u);
+    put_codes(t, w[0]);
+    if (t < MS_TERMS - 8) put_codes(t + 8, w[1]);
+    if (lane < MS_TERMS) put_scale((int)lane, finite || lane ? (uint32_t)max(e0 - 2 * (int)lane, 0) : 255u);
+}
 // A block of x with an infinity or a NaN has no terms but a scale that is not a number, so every sum that it enters comes out
 // as NaN: such a result is formed value by value from x itself (rare, and slow).
 __device__ __noinline__ float ms_redo(const MpParams& p, int m, int col) {
@@ -81,12 +123,20 @@ __global__ void __launch_bounds__(320, 2) mxfp_product_kernel(const __grid_const
     // pieces of scales that the tile's tokens lie in (t0 is a multiple of 128); past the last row there are none
     const int t_tiles = (int)min((long long)(p.o.nt + 127) / 128, ((long long)p.o.M * p.o.terms - t0 + 127) / 128);
 
+    float mine[MS_HERE];                                     // this warp's blocks of x, token by token within a step
+#pragma unroll
+    for (int i = 0; i < MS_HERE; ++i) {
+        const int k = k0 + (p.o.M == 1 ? i : i >> 1), m = p.o.M == 1 ? 0 : i & 1, col = k * MP_BK + (warp - 2) * MX_BLOCK + (int)(threadIdx.x & 31);
+        mine[i] = !p.here || warp < 2 || k >= k1 || col >= p.K ? 0.f
+                  : p.x_f32 ? static_cast<const float*>(p.x)[m * p.ldx + col] : __bfloat162float(static_cast<const bf16*>(p.x)[m * p.ldx + col]);
+    }
+
     if (threadIdx.x == 0) {
         abort_sh = 0;
-        for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, p.here ? 9 : 1); mbar_init(empty0 + 8 * s, 1); }
         mbar_init(accf, 1);
         fence_mbar_init();
-        tma_prefetch_desc(&map_a);
+        if (!p.here) tma_prefetch_desc(&map_a);
         tma_prefetch_desc(&map_b);
     }
     if (warp == 1) { tmem_alloc(smem_u32(&tmem_base_sh), p.tmem_cols); tmem_relinquish(); }
@@ -99,7 +149,7 @@ __global__ void __launch_bounds__(320, 2) mxfp_product_kernel(const __grid_const
     const uint32_t sf_at = MP_W_BYTES + p.x_bytes;
 
     if (warp == 0) {
-        const uint32_t bytes = MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (1 + t_tiles);
+        const uint32_t bytes = MP_W_BYTES + 2 * MX_SCALE_PIECE + (p.here ? 0u : p.x_bytes + 2 * MX_SCALE_PIECE * t_tiles);
         auto load_b = [&](int k, uint32_t s) {
             const uint32_t bar = full0 + 8 * s, dst = ring0 + s * p.stage_bytes;
             mbar_expect_tx(bar, bytes);
@@ -107,6 +157,7 @@ __global__ void __launch_bounds__(320, 2) mxfp_product_kernel(const __grid_const
             bulk_load_1d(dst + sf_at, p.b_scales + ((long long)wt * p.pieces + 2 * k) * MX_SCALE_PIECE, 2 * MX_SCALE_PIECE, bar);
         };
         auto load_a = [&](int k, uint32_t s) {
+            if (p.here) return;
             const uint32_t bar = full0 + 8 * s, dst = ring0 + s * p.stage_bytes;
             ml_tma_2d(dst + MP_W_BYTES, &map_a, bar, k * 128, t0);
             for (int i = 0; i < t_tiles; ++i)
@@ -160,10 +211,50 @@ __global__ void __launch_bounds__(320, 2) mxfp_product_kernel(const __grid_const
         if (elect_one()) umma_commit(accf);
         __syncwarp();
     }
+    if (p.here && warp >= 2) {
+        // the terms of a step's 256 columns, a block of 32 per warp, where copies would have put them
+        const int lane = threadIdx.x & 31, b = warp - 2;
+        uint32_t s = 0, ph = 1;
+#pragma unroll 1                                                // (once through little code: instructions come from L2 here)
+        for (int i = 0; i < MS_HERE; ++i) {
+            const int k = k0 + (p.o.M == 1 ? i : i >> 1), m = p.o.M == 1 ? 0 : i & 1;
+            if (k >= k1) break;
+            const float r = i < 2 ? (i == 0 ? mine[0] : mine[1]) : (i == 2 ? mine[2] : mine[3]);
+            if (m == 0 && !mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
+            const uint32_t tile = ring0 + s * p.stage_bytes + MP_W_BYTES, sf = ring0 + s * p.stage_bytes + sf_at + 2 * MX_SCALE_PIECE + (uint32_t)(b >> 2) * MX_SCALE_PIECE;
+            ms_terms(r,
+                     [&](int t, uint32_t word) {
+                         const uint32_t row = (uint32_t)(t * p.o.M + m);
+                         asm volatile("st.shared.b32 [%0], %1;" ::"r"(tile + row * 128u + (((uint32_t)b ^ (row & 7u)) << 4) + (uint32_t)(lane >> 3) * 4u), "r"(word) : "memory");
+                     },
+                     [&](int t, uint32_t scale) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(sf + mx_scale_at((uint32_t)(t * p.o.M + m), (uint32_t)b & 3u)), "r"(scale) : "memory"); });
+            if (m + 1 < p.o.M) continue;
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full0 + 8 * s);
+            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+        }
+    }
     mx_finish(p.o, tmem_base, smem, accf, abort_flag, wt, t0, rank, k1 - k0, false,
               [&](int m, int col, float v) { return p.o.terms > 1 && v != v ? ms_redo(p, m, col) : v; });
     drain_after_abort(abort_flag);
     if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
+}
+
+// One or two tokens whose terms are made in the product's own kernel, which saves a launch and the workspace: how many CTAs
+// share a reduction (two CTAs on each of 148 SMs), and whether what each has to make is little enough (a step of 256 columns and
+// one token is about 1000 clocks of 12 dependent rounds).
+constexpr int MS_HERE_CTAS = 296;
+inline int ms_here_split(int N, int K) {
+    const long long wts = ((long long)N + 127) / 128;
+    const int steps = (int)(((long long)K + MP_BK - 1) / MP_BK);
+    int split = 1;
+    while (split < 8 && split * 2 <= steps && wts * split * 2 <= MS_HERE_CTAS) split *= 2;
+    return split;
+}
+inline bool ms_here(int M, int N, int K) {
+    const int steps = (int)(((long long)K + MP_BK - 1) / MP_BK), split = ms_here_split(N, K);
+    return M <= 2 && M * ((steps + split - 1) / split) <= MS_HERE;
 }
 
 // Sizes and split of a call; terms > 1: A is a sum of so many matrices of o.M rows each, below one another.
@@ -184,7 +275,8 @@ inline bool mp_plan(MpParams& p, int K, int sms) {
     p.sf_col = (uint32_t)acc_cols;
     p.o.n_acc = acc_cols / p.o.nt < 3 ? acc_cols / p.o.nt : 3;
     p.o.split = 1;
-    while (p.o.split < 8 && p.o.split * 2 <= p.steps && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
+    if (p.here) p.o.split = ms_here_split(p.o.cols, K);
+    while (!p.here && p.o.split < 8 && p.o.split * 2 <= p.steps && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
     // fp32 results: at most 128 additions (of 64 products each) into an accumulator
     while (p.o.y_f32 && p.o.split < 8 && p.o.split * 2 <= p.steps && (long long)p.steps * 4 > 128LL * p.o.n_acc * p.o.split) p.o.split *= 2;
     p.stages = (int)((two ? (ML_SMEM_MOST - 4096) / 2 : ML_SMEM_MOST) / p.stage_bytes);
@@ -197,12 +289,7 @@ inline size_t mp_smem(const MpParams& p) {
     return 1024 + (ring > part ? ring : part);
 }
 
-// x [M][K], bf16 or fp32, as a sum of MS_TERMS matrices in MXFP4, term t in rows t M .. t M + M - 1: the first is x rounded, each
-// next one is what the ones before it leave, rounded with a scale of its own.  Every term takes at least two bits off the
-// largest of a block's 32 remainders (a value of [4, 8) units is at most 2 off, 1 up to 6), 2.6 of them on the average, so
-// the sum is x to 2^-24 of the largest of the 32: exact for bf16 values within 2^16 of each other.  With it the products of a
-// few tokens are block-scaled products of the codes of W as they are: nothing converts W, whose bytes are the floor.
-// A warp takes a block, a lane a value.
+// x [M][K] in MS_TERMS matrices (ms_terms), term t in rows t M .. t M + M - 1.  A warp takes a block.
 template <typename T>
 __global__ void __launch_bounds__(256) split_mxfp_kernel(const T* __restrict__ x, int M, int K, long long ldx, unsigned char* __restrict__ codes,
                                                          unsigned char* __restrict__ scales) {
@@ -212,28 +299,14 @@ __global__ void __launch_bounds__(256) split_mxfp_kernel(const T* __restrict__ x
     const int id = (int)((blockIdx.x * blockDim.x + threadIdx.x) >> 5), m = id / blocks, b = id - m * blocks;
     if (m >= M) return;
     const int col = b * MX_BLOCK + lane;
-    float r = col < K ? to_f32(x[m * ldx + col]) : 0.f;
-    const bool finite = !__any_sync(0xffffffffu, !(fabsf(r) < __uint_as_float(0x7f800000u)));
-    if (!finite) r = 0.f;
-#pragma unroll 1
-    for (int t = 0; t < MS_TERMS; ++t) {
-        const uint32_t ex = __reduce_max_sync(0xffffffffu, __float_as_uint(r) & 0x7fffffffu) >> 23;
-        const uint32_t s = ex > 2u ? ex - 2u : 0u;
-        uint32_t c;
-        asm("{\n .reg .b8 b0;\n cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n mov.b32 %0, {b0, b0, b0, b0};\n}"
-            : "=r"(c) : "f"(r * __uint_as_float((254u - s) << 23)), "f"(0.f));
-        c &= 15u;
-        const uint32_t mag = c & 7u;
-        const float v = mag < 2u ? 0.5f * (float)mag : __uint_as_float((mag + 252u) << 22);
-        r -= (c & 8u ? -v : v) * mx_scale_f32(s);            // exact: both are multiples of r's last bit, and the difference is smaller
-        uint32_t w = c << (4 * (lane & 7));
-        w |= __shfl_xor_sync(0xffffffffu, w, 1);
-        w |= __shfl_xor_sync(0xffffffffu, w, 2);
-        w |= __shfl_xor_sync(0xffffffffu, w, 4);
-        const int row = t * M + m;
-        if ((lane & 7) == 0 && b * 16 < row_bytes) *reinterpret_cast<uint32_t*>(codes + row * row_bytes + b * 16 + (lane >> 1)) = w;
-        if (lane == 0) scales[((long long)(row / MX_TILE) * pieces + b / 4) * MX_SCALE_PIECE + mx_scale_at((uint32_t)(row % MX_TILE), (uint32_t)b % 4u)] = finite || t ? (unsigned char)s : 255;
-    }
+    ms_terms(col < K ? to_f32(x[m * ldx + col]) : 0.f,
+             [&](int t, uint32_t word) {
+                 if (b * 16 < row_bytes) *reinterpret_cast<uint32_t*>(codes + (t * M + m) * row_bytes + b * 16 + (lane >> 3) * 4) = word;
+             },
+             [&](int t, uint32_t s) {
+                 const int row = t * M + m;
+                 scales[((long long)(row / MX_TILE) * pieces + b / 4) * MX_SCALE_PIECE + mx_scale_at((uint32_t)(row % MX_TILE), (uint32_t)b % 4u)] = (unsigned char)s;
+             });
 }
 // The workspace that holds the terms.
 struct MsSpace { long long codes, scales, bytes; };
