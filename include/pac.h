@@ -343,7 +343,8 @@ pac_status pac_dequantize_absmax(int device, void* cuda_stream, const signed cha
  *
  * These calls and those below enqueue on cuda_stream (NULL: the default stream) of `device`, leave the caller's current device
  * as it was, allocate nothing, keep nothing and may be captured into a graph.  No rows: nothing is done.  Errors:
- * PAC_ERR_INVALID_ARG for NULL or misaligned pointers, unknown types, cols < 1 or a pitch below it; PAC_ERR_CUDA. */
+ * PAC_ERR_INVALID_ARG for NULL or misaligned pointers, unknown types, cols < 1 or a pitch below it; PAC_ERR_UNSUPPORTED for more
+ * rows than a launch has tiles (some 16 million); PAC_ERR_CUDA.  Results do not overlap inputs. */
 pac_status pac_quantize_mxfp(int device, void* cuda_stream, const void* dev_x, int dtype, long long rows, int cols, long long ldx,
                              unsigned char* dev_codes, unsigned char* dev_scales);
 pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const unsigned char* dev_codes, const unsigned char* dev_scales,
@@ -387,7 +388,8 @@ pac_status pac_mxfp_product(int device, void* cuda_stream, const unsigned char* 
  * Pointers aligned to eight elements are the fast case, one element is enough.  step: the number of this step, from 1.
  * dev_step: device, its number there instead (read by the kernel; the caller moves it on), which a captured step needs: a
  * call under capture without it is refused with PAC_ERR_BAD_STATE.  hp, grad_scale and the list are as they were at capture.
- * Errors: PAC_ERR_INVALID_ARG for NULL or misaligned pointers, negative sizes, unknown types or bits, step < 1. */
+ * Errors: PAC_ERR_INVALID_ARG for NULL or misaligned pointers, negative sizes, unknown types or bits, step < 1
+ * (the number at dev_step is not looked at on the host). */
 typedef struct {
     void* p; const void* g;
     void* m; void* v;

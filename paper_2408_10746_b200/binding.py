@@ -567,6 +567,21 @@ def _out(out, rows: int, cols: int, dtype, device):
     return out, _rows(out, "out")[2]
 
 
+def _span(t):
+    """First and one-past-last address of a tensor's elements."""
+    a = t.data_ptr()
+    return a, a + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size() if t.numel() else a
+
+
+def _apart(out, *inputs):
+    """A result that the caller provides lies apart from what the call reads."""
+    a, b = _span(out)
+    for t in inputs:
+        c, d = _span(t)
+        if a < d and c < b:
+            _refuse("the result does not overlap the inputs")
+
+
 def quantize_mxfp(x, codes=None, scales=None):
     """(codes, scales) of a CUDA matrix, float32 or bfloat16, whose rows may lie apart: microscaled 4-bit floating point, one power
     of two per 32 columns.  Shapes as mxfp_shapes gives; codes and scales may be given to be written into."""
@@ -583,6 +598,8 @@ def quantize_mxfp(x, codes=None, scales=None):
         scales = torch.empty(shapes[1], dtype=torch.uint8, device=device) if scales is None else scales
         if _mxfp(codes, scales, cols, device) != rows:
             _refuse(f"codes have {rows} rows")
+        _apart(codes, x, scales)
+        _apart(scales, x)
     index = device.index
     st = load_library().pac_quantize_mxfp(index, _stream(index), x.data_ptr(), dtype, rows, cols, ld, codes.data_ptr(), scales.data_ptr())
     if st != 0:
@@ -597,6 +614,8 @@ def dequantize_mxfp(codes, scales, cols: int, dtype=None, out=None):
     device = codes.device
     dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
     code = _dtype(dtype)
+    if out is not None:
+        _apart(out, codes, scales)
     out, ld = _out(out, rows, cols, dtype, device)
     st = load_library().pac_dequantize_mxfp(device.index, _stream(device.index), codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), code, ld)
     if st != 0:
@@ -607,6 +626,8 @@ def dequantize_mxfp(codes, scales, cols: int, dtype=None, out=None):
 def _mxfp_linear(call, lib, x, M: int, ld: int, codes, scales, N: int, K: int, grad: bool, dtype, out):
     dtype = dtype or (out.dtype if out is not None else x.dtype)
     device, xt, yt, at = x.device, _dtype(x.dtype), _dtype(dtype), x.data_ptr()
+    if out is not None:
+        _apart(out, x, codes, scales)
     out, ldo = _out(out, M, K if grad else N, dtype, device)
     n = lib.pac_mxfp_linear_workspace(at, xt, M, ld, N, K, grad)
     space = codes.new_empty(n) if n else None
@@ -645,6 +666,8 @@ def mxfp_product(a_codes, a_scales, b_codes, b_scales, cols: int, dtype=None, ou
         _refuse("B has at least one row")
     dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
     code = _dtype(dtype)
+    if out is not None:
+        _apart(out, a_codes, a_scales, b_codes, b_scales)
     out, ldo = _out(out, M, N, dtype, device)
     st = load_library().pac_mxfp_product(device.index, _stream(device.index), a_codes.data_ptr(), a_scales.data_ptr(), M, b_codes.data_ptr(),
                                          b_scales.data_ptr(), N, cols, out.data_ptr(), code, ldo)
@@ -665,8 +688,8 @@ class AdamWTensors:
     """AdamW over a list of CUDA tensors (float32 or bfloat16, contiguous, all on one device) with moments in float32 (bits=32) or
     in 8 bits (bits=8: float8_e4m3fn codes, the second moment as its root, one float32 constant per 256 elements).
 
-    params and grads are borrowed; step() reads the grads and updates the params and the moments in place, in one launch on torch's
-    current stream.  state: dict of lists "m", "v" (and "m_scale", "v_scale"), made here as zeros when not given; state_lists()
+    params and grads are borrowed and stay where they are in memory (gradients are written into the same tensors step after step);
+    step() reads the grads and updates the params and the moments in place, in one launch on torch's current stream.  state: dict of lists "m", "v" (and "m_scale", "v_scale"), made here as zeros when not given; state_lists()
     returns it, which with `steps` is what a checkpoint has to keep.  decay: one truth value per tensor.  seed: names the random
     bits by which 8-bit codes are rounded."""
 

@@ -399,7 +399,8 @@ cudaError_t launch_adamw(cudaStream_t st, const pac_adamw_tensor* t, int count, 
 
 extern "C" pac_status pac_adamw_tensors(int device, void* cuda_stream, const pac_adamw_tensor* tensors, int count, int state_bits, const pac_adamw* hp,
                                         long long step, const long long* dev_step, float grad_scale, unsigned seed) {
-    if (count < 0 || !hp || (state_bits != 8 && state_bits != 32) || (count > 0 && !tensors) || (!dev_step && step < 1)) return PAC_ERR_INVALID_ARG;
+    if (count < 0 || !hp || (state_bits != 8 && state_bits != 32) || (count > 0 && !tensors) || (dev_step ? !aligned(dev_step, 8) : step < 1))
+        return PAC_ERR_INVALID_ARG;
     for (int i = 0; i < count; ++i) {
         const pac_adamw_tensor& t = tensors[i];
         if (t.n < 0 || t.n > (1LL << 39) || !dtype_ok(t.p_dtype) || !dtype_ok(t.g_dtype)) return PAC_ERR_INVALID_ARG;

@@ -351,14 +351,16 @@ def test_no_rows():
 def test_refusals():
     import paper_2408_10746_b200 as pac
     codes, scales, _ = matrix(40, 64, 1)
-    x = torch.randn(4, 64, device="cuda")
+    x, wide = torch.randn(4, 64, device="cuda"), torch.randn(4, 200, device="cuda")
     bad = [lambda: pac.mxfp_linear(x[:, :32], codes, scales), lambda: pac.mxfp_linear(x.half(), codes, scales), lambda: pac.mxfp_linear(x.t(), codes, scales),
            lambda: pac.mxfp_linear(x[0], codes, scales), lambda: pac.mxfp_linear(x, codes[:, :16], scales), lambda: pac.mxfp_linear(x, codes, scales[:, :1]),
            lambda: pac.mxfp_linear(x, codes.float(), scales), lambda: pac.mxfp_linear(x, codes, scales.cpu()), lambda: pac.mxfp_linear(x, codes, scales, torch.float16),
            lambda: pac.mxfp_linear(x, codes, scales, out=torch.empty(4, 41, device="cuda")), lambda: pac.mxfp_linear(x[:1].expand(4, 64), codes, scales),
            lambda: pac.mxfp_linear_grad(x, codes, scales, 64), lambda: pac.mxfp_linear_grad(x[:, :40], codes, scales, 96),
            lambda: pac.mxfp_product(codes, scales, codes, scales, 96), lambda: pac.quantize_mxfp(x.half()), lambda: pac.quantize_mxfp(x, codes=codes),
-           lambda: pac.dequantize_mxfp(codes, scales, 64, torch.float16), lambda: pac.quantize_mxfp(x.t())]
+           lambda: pac.dequantize_mxfp(codes, scales, 64, torch.float16), lambda: pac.quantize_mxfp(x.t()),
+           lambda: pac.mxfp_linear(wide[:, :64], codes, scales, out=wide[:, 30:70]), lambda: pac.mxfp_linear_grad(wide[:, :40], codes, scales, 64, out=wide[:, :64]),
+           lambda: pac.mxfp_product(codes[:4], scales, codes, scales, 64, out=codes.view(torch.bfloat16)[:4])]
     for i, call in enumerate(bad):
         with pytest.raises(pac.PacError) as e:
             call()
