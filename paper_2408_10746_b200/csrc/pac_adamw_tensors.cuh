@@ -5,7 +5,7 @@
 // 8 bits: m and sqrt(v) are kept as float8 (E4M3) times an fp32 constant per 256 elements, absmax / 448.  The root halves
 // the range of exponents that has to fit.  With beta2 = 0.999 a step moves v by a thousandth and neighbouring codes are
 // an eighth apart, so rounding to the nearest would hold v where it is for ever; codes are rounded up or down by 16
-// random bits instead (up with the probability of the remainder), which keeps the averages unbiased.  The bits are a hash
+// random bits instead (up with the probability of the remainder), which keeps what is stored unbiased.  The bits are a hash
 // of (seed, step, tensor, element): the same call gives the same codes.  A root that is not 0 never becomes 0, so a
 // moment never meets a denominator of eps alone.  A block with a gradient that is not finite gets the constant NaN.
 //
@@ -13,6 +13,9 @@
 // and gradients on top).  A warp takes 256 elements, eight per lane, so the block's maximum is five shuffles and the
 // moments never leave its registers between decoding and encoding.  The list is an argument of the kernel (constant
 // memory): nothing to copy, nothing to keep alive after the call, capturable.
+//
+// Measured, 202 M elements: 510 us with fp32 parameters and 8-bit moments (6.3 TB/s), 426 us with bf16 ones (4.7 TB/s: issue
+// slots, some 60 instructions an element); fp32 everywhere 50 M in 238 us (5.9 TB/s).
 #pragma once
 #include "pac_ptx.cuh"
 #include "pac_adamw.cuh"
@@ -193,7 +196,7 @@ __device__ __forceinline__ float at_warp_top(float top) { return __uint_as_float
 
 // 256 elements by a warp, eight consecutive ones per lane; all pointers aligned to eight elements.  What is read of a block,
 // as it lies in memory: the next block's are on their way while this one is computed (8 bits, 202 M bf16 elements: 697 us
-// without, see the note at the kernel).
+// without).
 template <int BITS, bool P16, bool G16>
 struct AtRaw {
     uint32_t p[P16 ? 4 : 8], g[G16 ? 4 : 8], m[BITS == 32 ? 8 : 2], v[BITS == 32 ? 8 : 2];

@@ -15,12 +15,16 @@
 // Few tiles: the reduction is split over a cluster, whose CTAs then add their partial sums through distributed shared
 // memory in the order of their ranks (no atomics, no workspace).
 //
+// What bounds it: converting, as long as there are few tokens to a tile.  A value costs two byte permutations, three masks or
+// shifts (a half-rate pipe) and half a product, so 32000 x 4096 takes 25 us of that pipe alone and 52 us in two uneven waves
+// of 250 CTAs (17 to 32 tokens; backward in one wave of split reductions 49); 4096 x 4096 takes 12 us.  From some 100 tokens on the
+// tensor cores: see pac_mxfp_pair.cuh.
+//
 // Precision: operands exact, sums in fp32.  The tensor core cuts partial sums instead of rounding them, so K steps take
 // turns over the accumulators that tensor memory has room for.  x in fp32 enters as three bf16 terms that add up to it
 // exactly; the second and third share an accumulator.
 #pragma once
 #include <cooperative_groups.h>
-#include <type_traits>
 
 #include "pac_mxfp.cuh"
 

@@ -5,6 +5,10 @@
 // bytes of a row = 256 values; bulk copies of the scales' pieces), tcgen05.cp spreads a piece over tensor memory (row r:
 // lane r % 32 of every quadrant, column r / 32, four scales to a 32-bit word), and no thread touches an operand.  As in
 // pac_mxfp_linear.cuh the frozen matrix is the M operand and the tokens are the N operand.
+//
+// What bounds it: up to 64 tokens the bytes of B (32000 x 4096: 12 us, floor 10.7), below some 10 MB of them the latency of one
+// CTA from set-up to stores (4096 x 4096: 7 us).  Up to 192 rows of A two CTAs share an SM, so that one's ring fills while the
+// other stores; 250 CTAs are then one wave.  Many tokens: pac_mxfp_product_pair.cuh.
 #pragma once
 #include "pac_mxfp_linear.cuh"
 
