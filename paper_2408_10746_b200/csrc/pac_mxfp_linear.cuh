@@ -415,25 +415,32 @@ mxfp_linear_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_c
     if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
 }
 
-// Tile, split and rings of one call; false when the sizes do not fit the grid.
+// Tile, split and rings of one call; false when the sizes do not fit the grid.  Tokens to a tile and the split of the reduction
+// by a model of a CTA's time in microseconds, times the waves: 2 to begin and end, 0.75 for each piece of W that it converts, and
+// per token of its tile 0.02, or 0.035 where the sum goes through the cluster.  (4096 x 4096 in 18.1, 24.6 and 32.5 us with 256
+// tokens in one tile and a split of four, 512 in two tiles and two, 512 in four tiles and none: 17, 23 and 29 by the model.)
+// Clusters of four and eight do not fill the last SMs of every group of them: 128 in all.
 inline bool ml_plan(MlParams& p, bool f32_terms, int sms) {
-    const int cap = f32_terms ? 64 : p.o.y_f32 ? 128 : 256;
-    const int tiles = (p.o.M + cap - 1) / cap;
-    p.o.nt = ((p.o.M + tiles - 1) / tiles + 15) / 16 * 16;
     const int wts = (int)(((long long)p.o.cols + 127) / 128);
-    const int tok_tiles = (p.o.M + p.o.nt - 1) / p.o.nt;
     p.red_tiles = (int)(((long long)p.red + 127) / 128);
-    p.o.n_acc = f32_terms ? 5 : (512 / p.o.nt < 4 ? 512 / p.o.nt : 4);
+    double best = 0;
+    for (int cap = f32_terms ? 64 : p.o.y_f32 ? 128 : 256; cap >= 64; cap /= 2) {
+        const int tiles = (p.o.M + cap - 1) / cap, nt = ((p.o.M + tiles - 1) / tiles + 15) / 16 * 16;
+        const int n_acc = f32_terms ? 5 : 512 / nt < 4 ? 512 / nt : 4, lead = f32_terms ? n_acc - 1 : n_acc;
+        const long long ctas = (long long)wts * ((p.o.M + nt - 1) / nt);
+        for (int split = 1; split <= 8 && split <= p.red_tiles; split *= 2) {
+            // fp32 results: at most 128 additions into an accumulator, as far as splitting goes
+            const bool more = split < 8 && split * 2 <= p.red_tiles;
+            if (p.o.y_f32 && more && (long long)p.red_tiles * 8 > 128LL * lead * split) continue;
+            const int at_once = split == 1 ? sms : split == 2 ? sms - 4 : sms * 7 / 8;
+            const double waves = (double)((ctas * split + at_once - 1) / at_once);
+            const double cost = waves * (2 + 0.75 * ((p.red_tiles + split - 1) / split) + nt * (split > 1 ? 0.035 : 0.02));
+            if (best == 0 || cost < best) { best = cost; p.o.nt = nt; p.o.split = split; p.o.n_acc = n_acc; }
+        }
+    }
+    const int tok_tiles = (p.o.M + p.o.nt - 1) / p.o.nt;
     p.tmem_cols = 32;
     while (p.tmem_cols < (uint32_t)(p.o.n_acc * p.o.nt)) p.tmem_cols *= 2;
-    // as many CTAs as there are SMs; fp32 results: at most 128 additions into an accumulator
-    p.o.split = 1;
-    const long long ctas = (long long)wts * tok_tiles;
-    while (p.o.split < 8 && p.o.split * 2 <= p.red_tiles && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
-    if (p.o.y_f32) {
-        const int lead = f32_terms ? p.o.n_acc - 1 : p.o.n_acc;
-        while (p.o.split < 8 && p.o.split * 2 <= p.red_tiles && (long long)p.red_tiles * 8 > 128LL * lead * p.o.split) p.o.split *= 2;
-    }
     p.stage_bytes = ML_A_BYTES + (uint32_t)p.o.nt * 128u * (f32_terms ? 3u : 1u);
     p.code_stages = p.o.nt > 128 ? 3 : 6;
     const size_t room = ML_SMEM_MOST - (size_t)p.code_stages * ((ML_CODE_BYTES + 127) / 128 * 128);

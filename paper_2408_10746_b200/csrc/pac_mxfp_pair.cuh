@@ -13,7 +13,7 @@
 
 namespace pac {
 
-constexpr int MR_STAGES = 6, MR_CODES = 3, MR_CONV_WARPS = 8, MR_EPI_WARPS = 4, MR_THREADS = 32 * (2 + MR_CONV_WARPS + MR_EPI_WARPS);
+constexpr int MR_STAGES = 6, MR_CODES = 3, MR_CONV_WARPS = 12, MR_EPI_WARPS = 4, MR_THREADS = 32 * (2 + MR_CONV_WARPS + MR_EPI_WARPS);
 constexpr uint32_t MR_STAGE = 2 * ML_A_BYTES;
 constexpr size_t MR_SMEM = 1024 + (size_t)MR_STAGES * MR_STAGE + (size_t)MR_CODES * ML_CODE_BYTES;
 
@@ -54,7 +54,7 @@ __device__ __forceinline__ bool mr_wait(uint32_t bar, uint32_t parity, volatile 
     return __all_sync(0xffffffffu, ok) != 0;
 }
 
-// Warps: 0 copies, 1 MMAs (of the pair's first CTA), 2-9 convert W, 10-13 store y.
+// Warps: 0 copies, 1 MMAs (of the pair's first CTA), 2-13 convert W, 14-17 store y.
 template <bool GRAD>
 __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_x,
                                                                          const __grid_constant__ MrParams p) {
@@ -73,8 +73,8 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
 
     if (threadIdx.x == 0) {
         abort_sh = 0;
-        for (int s = 0; s < MR_STAGES; ++s) { mbar_init(xfull0 + 8 * s, 1); mbar_init(afull0 + 8 * s, MR_CONV_WARPS); mbar_init(empty0 + 8 * s, 1); }
-        for (int s = 0; s < MR_CODES; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, MR_CONV_WARPS); }
+        for (int s = 0; s < MR_STAGES; ++s) { mbar_init(xfull0 + 8 * s, 1); mbar_init(afull0 + 8 * s, 8); mbar_init(empty0 + 8 * s, 1); }
+        for (int s = 0; s < MR_CODES; ++s) { mbar_init(cfull0 + 8 * s, 1); mbar_init(cempty0 + 8 * s, 8); }
         for (int b = 0; b < 2; ++b) { mbar_init(accf0 + 8 * b, 1); mbar_init(acce0 + 8 * b, 2 * MR_EPI_WARPS); }
         fence_mbar_init();
         tma_prefetch_desc(&map_codes);
@@ -154,31 +154,37 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
             }
         }
     } else if (warp < 2 + MR_CONV_WARPS) {
-        const int h = (warp - 2) >> 2, t = threadIdx.x - 64 - h * 128;
-        uint32_t cs = 0, cph = 0, s = (uint32_t)h, ph = 1;
+        // three groups of four warps, each with every third step of all this pair's tiles (six stages: its own are two of them)
+        constexpr uint32_t GROUPS = MR_CONV_WARPS / 4;
+        static_assert(MR_STAGES % GROUPS == 0, "a group's stages are its own");
+        const int g = (warp - 2) >> 2, t = (threadIdx.x - 64) & 127;
+        const int steps = 2 * p.terms * p.red_tiles, mine = unit0 < units ? (units - unit0 + unit_step - 1) / unit_step : 0;
+        const long long total = (long long)mine * steps;
+        uint32_t s = (uint32_t)g, ph = 1, cs = 0, cph = 0;    // cs: ring position of the piece that step n lies in
+        int i = g, c = 0;                                    // step within the tile; pieces passed
         const uint32_t afull_first = mapa_shared(afull0, 0u);
-        bool ok = true;
-        for (int u = unit0; u < units && ok; u += unit_step) {
-            for (int i = 0, kt = 0; i < p.terms * p.red_tiles && ok; ++i) {
-                ok = mbar_wait_uniform(cfull0 + 8 * cs, cph, abort_flag, nullptr);
-                if (!ok) break;
-                MlBlocks<GRAD> w;
-                w.load(codes0 + cs * ML_CODE_BYTES, t, h, kt, p.red);
-                uint32_t o[2][4][4];
-                w.convert(o);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(cempty0 + 8 * cs);
+        for (long long n = g; n < total; n += GROUPS) {
+            for (; c < (int)((n >> 1) & 0x7fffffff); ++c)
                 if (++cs == MR_CODES) { cs = 0; cph ^= 1u; }
-                ok = mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr);
-                if (!ok) break;
-                w.store(ring0 + s * MR_STAGE, t, h, o);
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mr_arrive(afull_first + 8 * s);
-                s += 2;
-                if (s >= MR_STAGES) { s = (uint32_t)h; ph ^= 1u; }
-                if (++kt == p.red_tiles) kt = 0;
-            }
+            while (i >= steps) i -= steps;
+            int kt = i >> 1;
+            while (kt >= p.red_tiles) kt -= p.red_tiles;
+            const int h = i & 1;
+            if (!mbar_wait_uniform(cfull0 + 8 * cs, cph, abort_flag, nullptr)) break;
+            MlBlocks<GRAD> w;
+            w.load(codes0 + cs * ML_CODE_BYTES, t, h, kt, p.red);
+            uint32_t o[2][4][4];
+            w.convert(o);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(cempty0 + 8 * cs);
+            if (!mbar_wait_uniform(empty0 + 8 * s, ph, abort_flag, nullptr)) break;
+            w.store(ring0 + s * MR_STAGE, t, h, o);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mr_arrive(afull_first + 8 * s);
+            s += GROUPS;
+            if (s >= MR_STAGES) { s = (uint32_t)g; ph ^= 1u; }
+            i += GROUPS;
         }
     } else {
         const int q = warp & 3;

@@ -263,11 +263,14 @@ inline bool ms_here(int M, int N, int K) {
 
 // Sizes and split of a call; terms > 1: A is a sum of so many matrices of o.M rows each, below one another.
 inline bool mp_plan(MpParams& p, int K, int sms) {
-    const int rows = p.o.M * p.o.terms, cap = p.o.y_f32 && p.o.terms == 1 ? 128 : 256;
+    const int rows = p.o.M * p.o.terms;
+    const long long wts = ((long long)p.o.cols + 127) / 128;
+    // 256 tokens to a tile where that gives every SM one (1000 x 4000, 512 tokens: 10 us with 128 to a tile, 22 with 256)
+    const int cap = p.o.terms == 1 && (p.o.y_f32 || wts * ((rows + 255LL) / 256) < sms) ? 128 : 256;
     // several token tiles begin at multiples of 128, where the pieces of scales do
     p.o.nt = rows <= cap ? (rows + 15) / 16 * 16 : cap;
     const int tok_tiles = (rows + p.o.nt - 1) / p.o.nt;
-    const long long wts = ((long long)p.o.cols + 127) / 128, ctas = wts * tok_tiles;
+    const long long ctas = wts * tok_tiles;
     p.steps = (int)(((long long)K + MP_BK - 1) / MP_BK);
     p.x_bytes = (uint32_t)p.o.nt * 128u;
     p.stage_bytes = MP_W_BYTES + p.x_bytes + 2 * MX_SCALE_PIECE * (uint32_t)(1 + (p.o.nt + 127) / 128);
