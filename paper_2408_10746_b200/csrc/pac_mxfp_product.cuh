@@ -8,7 +8,8 @@
 //
 // What bounds it: up to 64 tokens the bytes of B (32000 x 4096: 12 us, floor 10.7), below some 10 MB of them the latency of one
 // CTA from set-up to stores (4096 x 4096: 7 us).  Up to 192 rows of A two CTAs share an SM, so that one's ring fills while the
-// other stores; 250 CTAs are then one wave.  Many tokens: pac_mxfp_product_pair.cuh.
+// other stores; 250 CTAs are then one wave.  (Two tiles of B to a CTA that share the copies of A, one CTA to an SM: 26 us for 16 tokens
+// through 32000 x 4096 where this takes 24.)  Many tokens: pac_mxfp_product_pair.cuh.
 #pragma once
 #include "pac_mxfp_linear.cuh"
 

@@ -95,7 +95,7 @@ def test_rows_around_the_result_stay_as_they_were():
 
 
 # ---------------------------------------------------------------- products with x as it is
-SHAPES = [(1, 1, 1), (1, 4100, 2100), (2, 2500, 1000), (2, 64, 1500), (1, 40000, 300), (3, 300, 100), (1, 128, 128), (1, 130, 32), (2, 17, 33), (16, 128, 256), (17, 300, 770), (33, 129, 1000), (64, 1, 64), (65, 500, 129), (128, 128, 512),
+SHAPES = [(1, 1, 1), (1, 4100, 2100), (2, 2500, 1000), (2, 64, 1500), (1, 40000, 300), (3, 300, 100), (16, 23000, 520), (5, 24321, 250), (1, 128, 128), (1, 130, 32), (2, 17, 33), (16, 128, 256), (17, 300, 770), (33, 129, 1000), (64, 1, 64), (65, 500, 129), (128, 128, 512),
           (130, 257, 96), (256, 256, 1024), (257, 384, 640), (300, 1000, 250), (7, 64, 4096), (1, 2500, 1030)]
 
 
