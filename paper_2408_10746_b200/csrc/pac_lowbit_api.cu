@@ -250,7 +250,7 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     };
     const long long w_tiles = (out_cols + 127LL) / 128, units = (w_tiles + 1) / 2 * ((M + 255LL) / 256);
     // pairs where their tiles fill more than half of the SMs (4096 x 4096: 512 tokens, 32 tiles, 33 us in pairs and 25 in tiles of one CTA
-    // with a split reduction; 1024 tokens, 64 tiles, 34 in pairs and 43 so); fp32 results up to where two accumulators take 128
+    // with a split reduction; 1024 tokens, 64 tiles, 34 either way, 34 and 58 with fp32 results); fp32 results up to where two accumulators take 128
     // additions each
     if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (!y_f32 || red <= 4096)) {
         MrParams r = {};
@@ -345,7 +345,7 @@ extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsi
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
     const long long units = (N + 255LL) / 256 * ((M + 255LL) / 256);
-    // pairs where their tiles fill more than half of the SMs (4096 x 4096: 512 tokens 12 us either way, 1024 tokens 12 in pairs and 18 in
+    // pairs where their tiles fill more than half of the SMs (4096 x 4096: 512 tokens 12 us either way, 2048 tokens 19 in pairs and 26 in
     // tiles of one CTA); fp32 results up to 128 additions into an accumulator
     if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (y_dtype != PAC_F32 || K <= 8192)) {
         MqParams q = {};

@@ -6,8 +6,9 @@
 // additions into either).  An fp32 x comes as three bf16 terms and the reduction goes over W three times, the smallest term first: what
 // is cut off while the sums are small is smaller still.
 //
-// Measured: 8192 x 11008 x 4096 in 565 us (1.31 PFLOP/s, 0.93 of the library product's sustained rate), 650 us in runs of tenths of a
-// second, where the power cap sets the clock and converting has its share of the power.
+// Measured: 8192 x 11008 x 4096 in 530 us (1.39 PFLOP/s, 0.99 of the library product's sustained rate), 610 us in runs of tenths of a
+// second, where the power cap sets the clock and converting has its share of the power.  With two groups of converting warps
+// instead of three 565 us: a group's waits and fences take longer than two steps.
 #pragma once
 #include "pac_mxfp_linear.cuh"
 
