@@ -35,6 +35,12 @@ constexpr int ML_CONV_WARPS = 16;                            // in groups of fou
 constexpr uint32_t ML_A_BYTES = 128 * ML_BK * 2;
 constexpr uint32_t ML_CODE_BYTES = 128 * 64 + MX_SCALE_PIECE;
 constexpr int ML_MAX_STAGES = 8, ML_MAX_CODES = 8;
+// Pieces of codes in flight.  A group of converting warps has every second piece, so with an even number it meets a place of the
+// ring at every one of its fills, and the parity that it waits for is that of the fill it means; with an odd number it would
+// pass over fills, and a wait could be answered by the phase before the one that it passed over.
+constexpr int ML_CODES = 6, ML_CODES_WIDE = 2;
+static_assert(ML_CODES % (ML_CONV_WARPS / 8) == 0 && ML_CODES_WIDE % (ML_CONV_WARPS / 8) == 0 && ML_MAX_STAGES % (ML_CONV_WARPS / 4) == 0 && 4 % (ML_CONV_WARPS / 4) == 0,
+              "every group of converting warps meets its places of the rings at every fill");
 constexpr size_t ML_SMEM_MOST = 232448 - 1024 - 512;
 
 // What becomes of a product's accumulators (the block-scaled product's as well).
@@ -451,7 +457,7 @@ inline bool ml_plan(MlParams& p, bool f32_terms, int sms) {
     p.tmem_cols = 32;
     while (p.tmem_cols < (uint32_t)(p.o.n_acc * p.o.nt)) p.tmem_cols *= 2;
     p.stage_bytes = ML_A_BYTES + (uint32_t)p.o.nt * 128u * (f32_terms ? 3u : 1u);
-    p.code_stages = p.o.nt > 128 ? 3 : 6;
+    p.code_stages = p.o.nt > 128 ? ML_CODES_WIDE : ML_CODES;
     const size_t room = ML_SMEM_MOST - (size_t)p.code_stages * ((ML_CODE_BYTES + 127) / 128 * 128);
     p.stages = (int)(room / p.stage_bytes);
     p.stages = p.stages >= ML_MAX_STAGES ? ML_MAX_STAGES : 4;      // 4 or 8: a group of converters has every fourth

@@ -158,6 +158,9 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
         // three groups of four warps, each with every third step of all this pair's tiles (six stages: its own are two of them)
         constexpr uint32_t GROUPS = MR_CONV_WARPS / 4;
         static_assert(MR_STAGES % GROUPS == 0, "a group's stages are its own");
+        // of three pieces a group has a step in two, the same two places of a ring of three every time: it meets those at every
+        // fill, and the parities that it waits for are those of the fills it means
+        static_assert(MR_CODES == GROUPS && GROUPS == 3, "a group passes over no fill of its places");
         const int g = (warp - 2) >> 2, t = (threadIdx.x - 64) & 127;
         const int steps = 2 * p.terms * p.red_tiles, mine = unit0 < units ? (units - unit0 + unit_step - 1) / unit_step : 0;
         const long long total = (long long)mine * steps;
