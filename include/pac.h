@@ -351,9 +351,9 @@ pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const unsigned cha
                                long long rows, int cols, void* dev_out, int dtype, long long ldo);
 
 /* y = x W^T for a frozen matrix W [N][K] in MXFP4: dev_x [M][K], dev_y [M][N], either in fp32 or bf16 with any pitch and
- * alignment of an element.  The values of W enter exactly and sums are fp32; y is rounded once.  x enters exactly where there are
- * more than 16 tokens; up to 16 it enters as a sum of twelve MXFP4 matrices, to 2^-23 of the largest of the 32 neighbours in its
- * block (bf16 values within 2^14 of each other: exactly).  bf16 rows of x on 16-byte boundaries are the fast case.  Every
+ * alignment of an element.  The values of W enter exactly and sums are fp32; y is rounded once.  x enters exactly, but for one or
+ * two tokens, and up to 16 where W has 4 M values or more: there it may enter as a sum of twelve MXFP4 matrices, to 2^-23 of the
+ * largest of the 32 neighbours in its block (bf16 values within 2^14 of each other: exactly).  bf16 rows of x on 16-byte boundaries are the fast case.  Every
  * sum has a fixed order.  dev_workspace: 256-byte aligned, at least pac_mxfp_linear_workspace bytes, the call's own until its work is
  * done; NULL where that is 0.  Conventions as above.  (Waits inside the kernels are bounded; one that ran out, after about
  * a second, leaves NaN in its part of y.) */
@@ -364,8 +364,8 @@ pac_status pac_mxfp_linear(int device, void* cuda_stream, const void* dev_x, int
 pac_status pac_mxfp_linear_grad(int device, void* cuda_stream, const void* dev_dy, int dy_dtype, int M, long long lddy,
                                 const unsigned char* dev_codes, const unsigned char* dev_scales, int N, int K, void* dev_dx,
                                 int dx_dtype, long long lddx, void* dev_workspace, long long workspace_bytes);
-/* Bytes of workspace that a call with this x [M][K] (or dy [M][N], grad != 0) needs: up to 16 tokens for the terms of x (none for one
- * or two tokens and a W of moderate size), beyond that for bf16 terms of an fp32 x and for a bf16 x whose rows do not begin on
+/* Bytes of workspace that a call with this x [M][K] (or dy [M][N], grad != 0) needs: for the terms of x where it enters as such
+ * (see above; none for one or two tokens and a W of moderate size), else for bf16 terms of an fp32 x and for a bf16 x whose rows do not begin on
  * 16-byte boundaries; else 0.  Host arithmetic only. */
 long long pac_mxfp_linear_workspace(const void* dev_x, int x_dtype, int M, long long ldx, int N, int K, int grad);
 

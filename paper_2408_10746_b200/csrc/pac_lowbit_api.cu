@@ -201,13 +201,14 @@ cudaError_t launch_pair(int device, cudaStream_t st, const CUtensorMap& codes, c
     return cudaLaunchKernelEx(&cfg, kernel, codes, x, p);
 }
 
-// Terms of x instead of converting W (16 tokens: 10.8 us against 12 at 4096 x 4096, 20 against 52 at 32000 x 4096; twelve times 16
-// rows are what two CTAs on an SM have room for).
-bool few(bool grad, int M) { return !grad && M <= MS_MOST_TOKENS; }
+// Terms of x instead of converting W, up to 16 tokens (twelve times 16 rows are what two CTAs on an SM have room for): always where
+// they are made in the product's kernel, else from 4 M values of W on.  16 tokens: 10.8 us against 12 at 4096 x 4096, 20 against 52 at
+// 32000 x 4096; at 1000 x 770 8.4 against 7.6, and two launches to pay for instead of one.
+bool few(bool grad, int M, int N, int K) { return !grad && M <= MS_MOST_TOKENS && (ms_here(M, N, K) || (long long)N * K >= (4LL << 20)); }
 // Rows that TMA boxes can read as they are.
 bool boxes(const void* x, int dtype, long long ldx) { return dtype == PAC_BF16 && aligned(x, 16) && ldx % 8 == 0; }
 long long linear_space(bool grad, const void* x, int dtype, int M, long long ldx, int N, int K) {
-    if (few(grad, M)) return ms_here(M, N, K) ? 0 : ms_space(M, K).bytes;
+    if (few(grad, M, N, K)) return ms_here(M, N, K) ? 0 : ms_space(M, K).bytes;
     const int red = grad ? N : K;
     return boxes(x, dtype, ldx) ? 0 : (dtype == PAC_F32 ? 6LL : 2LL) * M * pack_columns(red);
 }
@@ -229,7 +230,7 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
         cudaGetLastError();
         return PAC_ERR_CUDA;
     };
-    if (few(grad, M)) return status(few_tokens(device, st, x, x_dtype, M, ldx, codes, scales, N, K, y, y_dtype, ldy, (unsigned char*)space));
+    if (few(grad, M, N, K)) return status(few_tokens(device, st, x, x_dtype, M, ldx, codes, scales, N, K, y, y_dtype, ldy, (unsigned char*)space));
     const int sms = sm_count(device), terms = x_dtype == PAC_F32 ? 3 : 1;
     const bool y_f32 = y_dtype == PAC_F32;
     long long x_cols = red, x_pitch = ldx;

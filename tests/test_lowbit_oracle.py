@@ -106,8 +106,8 @@ def test_bad_arguments_of_the_c_calls_are_refused_before_any_device_is_touched()
     # workspaces: terms of few tokens, packed copies of what boxes cannot read, none for aligned bf16
     assert lib.pac_mxfp_linear_workspace(ok, 1, 17, 64, 64, 64, 0) == 0 == lib.pac_mxfp_linear_workspace(ok, 1, 3, 64, 64, 64, 1)
     assert lib.pac_mxfp_linear_workspace(ok, 1, 17, 65, 64, 64, 0) == 17 * 128 * 2 == lib.pac_mxfp_linear_workspace(ok + 2, 1, 17, 64, 64, 64, 1)
-    assert lib.pac_mxfp_linear_workspace(ok, 0, 17, 64, 130, 64, 1) == 17 * 256 * 6 and lib.pac_mxfp_linear_workspace(ok, 1, 3, 64, 64, 64, 0) > 0
-    assert lib.pac_mxfp_linear_workspace(ok, 1, 1, 64, 64, 64, 0) == 0 and lib.pac_mxfp_linear_workspace(ok, 1, 1, 4096, 32000, 4096, 0) > 0
+    assert lib.pac_mxfp_linear_workspace(ok, 0, 17, 64, 130, 64, 1) == 17 * 256 * 6 and lib.pac_mxfp_linear_workspace(ok, 1, 3, 4096, 4096, 4096, 0) > 0
+    assert lib.pac_mxfp_linear_workspace(ok, 1, 1, 64, 64, 64, 0) == 0 == lib.pac_mxfp_linear_workspace(ok, 1, 3, 64, 64, 64, 0) and lib.pac_mxfp_linear_workspace(ok, 1, 1, 4096, 32000, 4096, 0) > 0
     for space, n in ((None, 0), (ok, 17 * 128 * 6 - 1), (ok + 16, 1 << 20)):
         assert lib.pac_mxfp_linear(0, None, ok, 0, 17, 64, ok, ok, 64, 64, ok, 0, 64, space, n) == 1
     assert lib.pac_mxfp_product(0, None, ok, ok, 4, ok, ok + 1, 64, 64, ok, 0, 64) == 1

@@ -95,7 +95,7 @@ def test_rows_around_the_result_stay_as_they_were():
 
 
 # ---------------------------------------------------------------- products with x as it is
-SHAPES = [(1, 1, 1), (1, 4100, 2100), (2, 2500, 1000), (2, 64, 1500), (1, 40000, 300), (3, 300, 100), (16, 23000, 520), (5, 24321, 250), (1, 128, 128), (1, 130, 32), (2, 17, 33), (16, 128, 256), (17, 300, 770), (33, 129, 1000), (64, 1, 64), (65, 500, 129), (128, 128, 512),
+SHAPES = [(1, 1, 1), (1, 4100, 2100), (2, 2500, 1000), (2, 64, 1500), (1, 40000, 300), (3, 300, 100), (16, 23000, 520), (5, 24321, 250), (12, 1100, 4100), (1, 128, 128), (1, 130, 32), (2, 17, 33), (16, 128, 256), (17, 300, 770), (33, 129, 1000), (64, 1, 64), (65, 500, 129), (128, 128, 512),
           (130, 257, 96), (256, 256, 1024), (257, 384, 640), (300, 1000, 250), (7, 64, 4096), (1, 2500, 1030)]
 
 
@@ -184,11 +184,12 @@ def test_not_a_number_stays_in_its_row_or_column(which):
         assert y[[7, 9]].isnan().all() and y[:7].isfinite().all() and y[10:].isfinite().all()
 
 
+@pytest.mark.parametrize("n", [300, 4000])                        # W converted; x as terms
 @pytest.mark.parametrize("xt", ["bf16", "f32"])
-def test_few_tokens_with_values_that_are_not_finite_and_of_all_sizes(xt):
+def test_few_tokens_with_values_that_are_not_finite_and_of_all_sizes(xt, n):
     """Up to 16 tokens x is a sum of twelve 4-bit matrices: to 2^-23 of the largest of 32 neighbours; infinities and NaN as ever."""
     import paper_2408_10746_b200 as pac
-    codes, scales, w = matrix(300, 1100, 21)
+    codes, scales, w = matrix(n, 1100, 21)
     g = torch.Generator().manual_seed(3)
     x = (torch.randn(16, 1100, generator=g) * torch.exp2(torch.randint(-30, 30, (16, 1100), generator=g).float())).to(TYPES[xt]).cuda()
     x[3] = 0
@@ -196,13 +197,13 @@ def test_few_tokens_with_values_that_are_not_finite_and_of_all_sizes(xt):
     near = host(x)
     top = np.abs(np.pad(near, ((0, 0), (0, 20)))).reshape(16, 35, 32).max(2).repeat(32, 1)[:, :1100]
     y = pac.mxfp_linear(x, codes, scales, torch.float32)
-    tol = bound(near @ w.T, np.abs(near) @ np.abs(w.T), 1100 / 64 + 16 + 12, torch.float32) + 2.0 ** -23 * (top @ np.abs(w.T))
+    tol = bound(near @ w.T, np.abs(near) @ np.abs(w.T), 1100 / 16 + 16, torch.float32) + 2.0 ** -23 * (top @ np.abs(w.T))
     assert (np.abs(host(y) - near @ w.T) <= tol).all()
     for m in (1, 2):                                             # the terms are made in the product's kernel there
         assert (np.abs(host(pac.mxfp_linear(x[4:4 + m], codes, scales, torch.float32)) - near[4:4 + m] @ w.T) <= tol[4:4 + m]).all()
     x[2, 500], x[7, 0], x[9, 1099] = float("inf"), float("nan"), -float("inf")
     x[9, 3] = float("inf")
-    got, want = host(pac.mxfp_linear(x, codes, scales, torch.float32)), (host(x)[:, None, :] * w[None]).sum(2)
+    got, want = host(pac.mxfp_linear(x, codes, scales, torch.float32)), np.stack([(row * w).sum(1) for row in host(x)])
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want))
     assert np.array_equal(np.sign(got[np.isinf(got)]), np.sign(want[np.isinf(want)]))
     for m in (2, 7, 8):
@@ -286,13 +287,14 @@ def test_every_scale_and_every_pair_of_codes_in_the_block_scaled_product(n):
 
 
 # ---------------------------------------------------------------- the calls themselves
-def test_calls_repeat_bit_for_bit_and_are_captured():
+@pytest.mark.parametrize("M,N,dtype", [(50, 700, torch.bfloat16), (50, 700, torch.float32), (1, 700, torch.bfloat16), (7, 5000, torch.bfloat16), (600, 5000, torch.float32)])
+def test_calls_repeat_bit_for_bit_and_are_captured(M, N, dtype):
     import paper_2408_10746_b200 as pac
-    codes, scales, w = matrix(700, 900, 6)
-    x = torch.randn(50, 900, device="cuda").bfloat16()
-    dy = torch.randn(50, 700, device="cuda").bfloat16()
-    y, dx, q = (torch.empty(s, device="cuda") for s in ((50, 700), (50, 900), (50, 700)))
-    xc, xs = (torch.empty(s, dtype=torch.uint8, device="cuda") for s in pac.mxfp_shapes(50, 900))
+    codes, scales, w = matrix(N, 900, 6)
+    x = torch.randn(M, 900, device="cuda").to(dtype)
+    dy = torch.randn(M, N, device="cuda").to(dtype)
+    y, dx, q = (torch.empty(s, device="cuda") for s in ((M, N), (M, 900), (M, N)))
+    xc, xs = (torch.empty(s, dtype=torch.uint8, device="cuda") for s in pac.mxfp_shapes(M, 900))
 
     def calls():
         pac.mxfp_linear(x, codes, scales, out=y)
@@ -310,8 +312,8 @@ def test_calls_repeat_bit_for_bit_and_are_captured():
         calls()
     for seed in (1, 2):
         torch.manual_seed(seed)
-        x.copy_(torch.randn(50, 900))
-        dy.copy_(torch.randn(50, 700))
+        x.copy_(torch.randn(M, 900))
+        dy.copy_(torch.randn(M, N))
         calls()
         want = [t.clone() for t in (y, dx, q)]
         for t in (y, dx, q):
@@ -322,8 +324,8 @@ def test_calls_repeat_bit_for_bit_and_are_captured():
 
 def test_two_streams_at_once():
     import paper_2408_10746_b200 as pac
-    mats = [matrix(300 + 64 * i, 512, i) for i in range(2)]
-    xs = [torch.randn(30, 512, device="cuda").bfloat16() for _ in range(2)]
+    mats = [matrix(n, 512, i) for i, n in enumerate((300, 9000))]
+    xs = [torch.randn(m, 512, device="cuda").bfloat16() for m in (30, 9)]
     want = [pac.mxfp_linear(x, m[0], m[1]) for x, m in zip(xs, mats)]
     streams = [torch.cuda.Stream() for _ in range(2)]
     got = [[], []]
