@@ -14,8 +14,8 @@
 // moments never leave its registers between decoding and encoding.  The list is an argument of the kernel (constant
 // memory): nothing to copy, nothing to keep alive after the call, capturable.
 //
-// Measured, 202 M elements: 510 us with fp32 parameters and 8-bit moments (6.3 TB/s), 426 us with bf16 ones (4.7 TB/s: issue
-// slots, some 60 instructions an element); fp32 everywhere 50 M in 238 us (5.9 TB/s).
+// Measured, 202 M elements: 510 us with fp32 parameters and 8-bit moments (6.3 TB/s), 426 us with bf16 ones (4.7 TB/s: half
+// the bytes in flight for the same 60 instructions an element; two blocks ahead do not fit the registers, 487 us and more); fp32 everywhere 50 M in 238 us (5.9 TB/s).
 #pragma once
 #include "pac_ptx.cuh"
 #include "pac_adamw.cuh"
