@@ -205,6 +205,11 @@ cudaError_t launch_pair(int device, cudaStream_t st, const CUtensorMap& codes, c
 // they are made in the product's kernel, else from 4 M values of W on.  16 tokens: 10.8 us against 12 at 4096 x 4096, 20 against 52 at
 // 32000 x 4096; at 1000 x 770 8.4 against 7.6, and two launches to pay for instead of one.
 bool few(bool grad, int M, int N, int K) { return !grad && M <= MS_MOST_TOKENS && (ms_here(M, N, K) || (long long)N * K >= (4LL << 20)); }
+// Steps to each of as few equal parts as have at most `most`.
+int equal_part(long long steps, int most) {
+    const long long parts = (steps + most - 1) / most;
+    return (int)((steps + parts - 1) / parts);
+}
 // Rows that TMA boxes can read as they are.
 bool boxes(const void* x, int dtype, long long ldx) { return dtype == PAC_BF16 && aligned(x, 16) && ldx % 8 == 0; }
 long long linear_space(bool grad, const void* x, int dtype, int M, long long ldx, int N, int K) {
@@ -260,6 +265,7 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
         r.w_tiles = (int)w_tiles; r.w_units = (int)((w_tiles + 1) / 2); r.t_units = (int)((M + 255LL) / 256);
         r.n_acc = y_f32 ? 2 : 1;
         r.terms = terms; r.x_rows = M;
+        r.part = y_f32 ? 2 * terms * r.red_tiles : equal_part(2LL * terms * r.red_tiles, MX_ADDS_BF16 / 4);
         if (!map_x(128)) return PAC_ERR_CUDA;
         return status(grad ? launch_pair<true>(device, st, mc, mx, r, sms) : launch_pair<false>(device, st, mc, mx, r, sms));
     }
@@ -352,6 +358,7 @@ extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsi
         MqParams q = {};
         q.y = dev_y; q.ldy = ldy; q.y_f32 = y_dtype == PAC_F32; q.M = M; q.cols = N; q.steps = (int)((K + 255LL) / 256);
         q.w_units = (int)((N + 255LL) / 256); q.t_units = (int)((M + 255LL) / 256);
+        q.part = y_dtype == PAC_F32 ? q.steps : equal_part(q.steps, MX_ADDS_BF16 / 4);
         e = launch_product_pair(device, st, dev_a_codes, dev_a_scales, dev_b_codes, dev_b_scales, K, q, sms);
         if (e == cudaSuccess) return PAC_OK;
         cudaGetLastError();

@@ -42,6 +42,11 @@ constexpr int ML_CODES = 6, ML_CODES_WIDE = 2;
 static_assert(ML_CODES % (ML_CONV_WARPS / 8) == 0 && ML_CODES_WIDE % (ML_CONV_WARPS / 8) == 0 && ML_MAX_STAGES % (ML_CONV_WARPS / 4) == 0 && 4 % (ML_CONV_WARPS / 4) == 0,
               "every group of converting warps meets its places of the rings at every fill");
 constexpr size_t ML_SMEM_MOST = 232448 - 1024 - 512;
+// Additions (of 16 products each, 64 in the block-scaled product) that an accumulator takes: each cuts up to 2^-23 of the sum, always
+// towards zero, so the cuts add up over the length of a reduction.  128 take at most 2^-16 of the sums from an fp32 result, 512 at
+// most 2^-14 from a bf16 one, a 64th of the half step that it is rounded by.  (All 2000 of a gradient over 32000 rows in one:
+// 1.4 in 1000 of its bf16 values on the other side of the exact one's rounding, 0.4 in 1000 so, 0.2 in 1000 of an fp32 sum's.)
+constexpr int MX_ADDS_F32 = 128, MX_ADDS_BF16 = 512;
 
 // What becomes of a product's accumulators (the block-scaled product's as well).
 struct MxOut {
@@ -444,9 +449,9 @@ inline bool ml_plan(MlParams& p, bool f32_terms, int sms) {
         const int n_acc = f32_terms ? 5 : 512 / nt < 4 ? 512 / nt : 4, lead = f32_terms ? n_acc - 1 : n_acc;
         const long long ctas = (long long)wts * ((p.o.M + nt - 1) / nt);
         for (int split = 1; split <= 8 && split <= p.red_tiles; split *= 2) {
-            // fp32 results: at most 128 additions into an accumulator, as far as splitting goes
+            // the additions into an accumulator, as far as splitting goes
             const bool more = split < 8 && split * 2 <= p.red_tiles;
-            if (p.o.y_f32 && more && (long long)p.red_tiles * 8 > 128LL * lead * split) continue;
+            if (more && (long long)p.red_tiles * 8 > (long long)(p.o.y_f32 ? MX_ADDS_F32 : MX_ADDS_BF16) * lead * split) continue;
             const int at_once = split == 1 ? sms : split == 2 ? sms - 4 : sms * 7 / 8;
             const double waves = (double)((ctas * split + at_once - 1) / at_once);
             const double cost = waves * (2 + 0.75 * ((p.red_tiles + split - 1) / split) + nt * (split > 1 ? 0.035 : 0.02));

@@ -3,7 +3,8 @@
 // converted once per 256 tokens and a K step of 64 costs an SM 8192 conversions and 20 KB from L2 for 512 clocks of tensor work;
 // alone it would be the same conversions and 36 KB.  Persistent pairs; the accumulators of one tile are stored while the
 // next tile is computed (bf16 results), or both halves of tensor memory take turns within a tile (fp32 results: half the
-// additions into either).  An fp32 x comes as three bf16 terms and the reduction goes over W three times, the smallest term first: what
+// additions into either).  A reduction of more additions than a bf16 result's accumulator takes is computed in equal parts: one
+// half of tensor memory receives a part, the storing warps add it to the sum of the parts before it, which the other half holds.  An fp32 x comes as three bf16 terms and the reduction goes over W three times, the smallest term first: what
 // is cut off while the sums are small is smaller still.
 //
 // Measured: 8192 x 11008 x 4096 in 530 us (1.39 PFLOP/s, 0.99 of the library product's sustained rate), 610 us in runs of tenths of a
@@ -25,6 +26,7 @@ struct MrParams {
     int w_tiles;                                            // 128-wide tiles of y's columns
     int w_units, t_units;                                   // pairs of them; tiles of 256 tokens
     int n_acc;                                              // accumulators per tile: 1 (two tiles in flight) or 2
+    int part;                                               // K steps to a part of the reduction (n_acc 2: all of them)
     int terms, x_rows;                                      // x is the sum of so many matrices of x_rows rows, the last ones (the small ones) first
 };
 
@@ -126,15 +128,17 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
             const uint32_t idesc = instr_desc_bf16(256, 256, GRAD ? 1 : 0, 0);
             const uint64_t a0 = GRAD ? smem_desc_sw128(ring0, 8192, 1024) : smem_desc_sw128(ring0, 16, 1024);
             const uint64_t b0 = smem_desc_sw128(ring0 + ML_A_BYTES, 16, 1024), astep = GRAD ? 128u : 2u;
-            uint32_t s = 0, ph = 0, tile = 0;
+            const int steps = 2 * p.terms * p.red_tiles, parts = (steps + p.part - 1) / p.part, n = ((units - unit0 + unit_step - 1) / unit_step) * parts;
+            const bool turns = p.n_acc == 1 && parts == 1;   // tiles in both halves of tensor memory by turns
+            uint32_t s = 0, ph = 0;
             bool ok = true;
-            for (int u = unit0; u < units && ok; u += unit_step, ++tile) {
-                const uint32_t buf = p.n_acc == 1 ? tile & 1u : 0u, use = p.n_acc == 1 ? tile >> 1 : tile;
+            for (int fill = 0, i0 = 0; fill < n && ok; ++fill) {
+                const uint32_t buf = turns ? (uint32_t)fill & 1u : 0u, use = turns ? (uint32_t)fill >> 1 : (uint32_t)fill;
                 ok = mr_wait(acce0 + 8 * buf, (use & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                const int steps = 2 * p.terms * p.red_tiles;
-                for (int i = 0; i < steps; ++i) {
+                const int here = min(p.part, steps - i0);
+                for (int i = 0; i < here; ++i) {
                     ok = mr_wait(xfull0 + 8 * s, ph, abort_flag) && mr_wait(afull0 + 8 * s, ph, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
@@ -152,6 +156,7 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
                 if (!ok) break;
                 if (elect_one()) umma_commit_pair(accf0 + 8 * buf, (uint16_t)3);
                 __syncwarp();
+                i0 = i0 + here == steps ? 0 : i0 + here;
             }
         }
     } else if (warp < 2 + MR_CONV_WARPS) {
@@ -193,13 +198,42 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
     } else {
         const int q = warp & 3;
         const uint32_t acce_first = mapa_shared(acce0, 0u), taddr = tmem_base + ((uint32_t)(q * 32) << 16);
-        uint32_t tile = 0;
+        const int steps = 2 * p.terms * p.red_tiles, parts = (steps + p.part - 1) / p.part;
+        const bool turns = p.n_acc == 1 && parts == 1;
+        uint32_t fill = 0;
         bool ok = true;
-        for (int u = unit0; u < units; u += unit_step, ++tile) {
+        for (int u = unit0; u < units; u += unit_step) {
             const int col = ((u % p.w_units) * 2 + (int)rank) * 128 + q * 32 + lane, t0 = (u / p.w_units) * 256;
-            const uint32_t buf = p.n_acc == 1 ? tile & 1u : 0u, use = p.n_acc == 1 ? tile >> 1 : tile;
-            ok = ok && mr_wait(accf0 + 8 * buf, use & 1u, abort_flag);
-            tc_fence_after();
+            if (parts > 1) {
+                // the MMAs wait meanwhile, once in 65000 clocks (2048 tokens, 32000 x 4096: 450-459 us in long runs, 454-497 with all
+                // additions in one accumulator); only this warp touches its lanes of the sum
+                for (int part = 0; part < parts; ++part, ++fill) {
+                    ok = ok && mr_wait(accf0, fill & 1u, abort_flag);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c0 = 0; c0 < 256; c0 += 16) {
+                        float v[16], w[16];
+                        tmem_ld16(taddr + c0, v);
+                        if (part) tmem_ld16(taddr + 256u + c0, w);
+                        tmem_ld_wait();
+                        if (part) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) v[e] += w[e];
+                        }
+                        tmem_st16(taddr + 256u + c0, v);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(acce_first);
+                }
+            }
+            const uint32_t buf = parts > 1 ? 1u : turns ? fill & 1u : 0u;
+            if (parts == 1) {
+                ok = ok && mr_wait(accf0 + 8 * buf, (turns ? fill >> 1 : fill) & 1u, abort_flag);
+                tc_fence_after();
+                ++fill;
+            }
             const int n_tok = min(256, p.M - t0);
             for (int c0 = 0; c0 < 256; c0 += 16) {
                 float v[16], w[16];
@@ -219,6 +253,7 @@ __global__ void __launch_bounds__(MR_THREADS, 1) mxfp_linear_pair_kernel(const _
                     else mx_store16(static_cast<bf16*>(p.y) + (long long)(t0 + c0) * p.ldy + col, p.ldy, n_tok - c0, v);
                 }
             }
+            if (parts > 1) continue;                         // (handed back above)
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(acce_first + 8 * buf);

@@ -285,8 +285,8 @@ inline bool mp_plan(MpParams& p, int K, int sms) {
     p.o.split = 1;
     if (p.here) p.o.split = ms_here_split(p.o.cols, K);
     while (!p.here && p.o.split < 8 && p.o.split * 2 <= p.steps && ctas * p.o.split * 2 <= sms) p.o.split *= 2;
-    // fp32 results: at most 128 additions (of 64 products each) into an accumulator
-    while (p.o.y_f32 && p.o.split < 8 && p.o.split * 2 <= p.steps && (long long)p.steps * 4 > 128LL * p.o.n_acc * p.o.split) p.o.split *= 2;
+    // the additions into an accumulator, as far as splitting goes
+    while (p.o.split < 8 && p.o.split * 2 <= p.steps && (long long)p.steps * 4 > (long long)(p.o.y_f32 ? MX_ADDS_F32 : MX_ADDS_BF16) * p.o.n_acc * p.o.split) p.o.split *= 2;
     p.stages = (int)((two ? (ML_SMEM_MOST - 4096) / 2 : ML_SMEM_MOST) / p.stage_bytes);
     if (p.stages > MP_MAX_STAGES) p.stages = MP_MAX_STAGES;
     return wts * p.o.split <= 0x7fffffffLL && tok_tiles <= 65535;

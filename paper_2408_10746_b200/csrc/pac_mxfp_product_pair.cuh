@@ -3,7 +3,8 @@
 // (codes of its own 128 rows and of half of the tokens, scales of its own rows and of all the tokens), close to the 64 bytes per
 // clock that an SM receives from L2; a CTA alone brings in 51 KB.  Tensor memory holds one accumulator of 256 columns beside the
 // scales, so the eight storing warps take a finished tile into registers at once (128 values a thread) and hand it back before
-// they store, while the next tile's copies are already in the ring.
+// they store, while the next tile's copies are already in the ring.  A reduction of more additions than an accumulator takes
+// (MX_ADDS_BF16) comes in equal parts, which are added up in those registers.
 //
 // Measured: 8192 x 11008 x 4096 in some 145 us (5 PFLOP/s; a CTA alone on 128 x 256 tiles, one after another: 315 us).
 #pragma once
@@ -21,6 +22,7 @@ constexpr uint32_t MQ_SF_COL = 256;
 struct MqParams {
     void* y; long long ldy; int y_f32;
     int M, cols, steps;                                     // steps of 256 values
+    int part;                                               // steps to a part of the reduction
     int w_units, t_units;
 };
 
@@ -95,13 +97,15 @@ mxfp_product_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
             const uint32_t idesc0 = instr_desc_mxf4(256, 256, 0u), idesc1 = instr_desc_mxf4(256, 256, 2u);
             const uint64_t w0 = smem_desc_sw128(ring0, 16, 1024), x0 = smem_desc_sw128(ring0 + MP_W_BYTES, 16, 1024);
             const uint64_t wf0 = smem_desc_plain(ring0 + MQ_W_SF), xf0 = smem_desc_plain(ring0 + MQ_X_SF);
-            uint32_t s = 0, ph = 0, tile = 0, set = 0;
+            const int n = ((units - unit0 + unit_step - 1) / unit_step) * ((p.steps + p.part - 1) / p.part);
+            uint32_t s = 0, ph = 0, set = 0;
             bool ok = true;
-            for (int u = unit0; u < units && ok; u += unit_step, ++tile) {
-                ok = mr_wait(acce, (tile & 1u) ^ 1u, abort_flag);
+            for (int fill = 0, i0 = 0; fill < n && ok; ++fill) {
+                ok = mr_wait(acce, ((uint32_t)fill & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                for (int i = 0; i < p.steps; ++i) {
+                const int here = min(p.part, p.steps - i0);
+                for (int i = 0; i < here; ++i) {
                     ok = mr_wait(full0 + 8 * s, ph, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
@@ -126,24 +130,38 @@ mxfp_product_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
                 if (!ok) break;
                 if (elect_one()) umma_commit_pair(accf, (uint16_t)3);
                 __syncwarp();
+                i0 = i0 + here == p.steps ? 0 : i0 + here;
             }
         }
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t acce_first = mapa_shared(acce, 0u), taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)half * 128u;
-        uint32_t tile = 0;
+        uint32_t fill = 0;
         bool ok = true;
-        for (int u = unit0; u < units; u += unit_step, ++tile) {
+        for (int u = unit0; u < units; u += unit_step) {
             const int col = ((u % p.w_units) * 2 + (int)rank) * 128 + q * 32 + lane, t0 = (u / p.w_units) * 256 + half * 128;
-            ok = ok && mr_wait(accf, tile & 1u, abort_flag);
-            tc_fence_after();
             float v[8][16];
+            for (int i0 = 0; i0 < p.steps; i0 += p.part, ++fill) {
+                ok = ok && mr_wait(accf, fill & 1u, abort_flag);
+                tc_fence_after();
+                if (i0 == 0) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) tmem_ld16(taddr + c * 16, v[c]);
-            tmem_ld_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(acce_first);
+                    for (int c = 0; c < 8; ++c) tmem_ld16(taddr + c * 16, v[c]);
+                    tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        float w[8];                          // (what is left of the registers)
+                        tmem_ld8(taddr + c * 8, w);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[c >> 1][(c & 1) * 8 + e] += w[e];
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acce_first);
+            }
             if (!ok) {                                       // a wait that ran out leaves NaN, not a wrong number
 #pragma unroll
                 for (int c = 0; c < 128; ++c) v[c >> 4][c & 15] = __uint_as_float(0x7fffffffu);
