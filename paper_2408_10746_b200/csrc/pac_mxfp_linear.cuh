@@ -188,6 +188,8 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
     else __syncthreads();
     const int g0 = (int)((long long)groups * rank / o.split), g1 = (int)((long long)groups * (rank + 1) / o.split);
     for (int i = g0 + (int)threadIdx.x; i < g1; i += (int)blockDim.x) {
+        const int c = i >> 5, col = wt * 128 + (i & 31) * 4;
+        if (col >= o.cols) continue;                         // before anything is loaded: see the end
         float4 v;
         switch (o.split) {                                   // all ranks' parts are asked for before the first is added
             case 2: v = sum_ranks<2>(cluster, part, i); break;
@@ -195,7 +197,6 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
             case 8: v = sum_ranks<8>(cluster, part, i); break;
             default: v = part[i];
         }
-        const int c = i >> 5, col = wt * 128 + (i & 31) * 4;
         const float w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -206,8 +207,9 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
             else static_cast<bf16*>(o.y)[at] = __float2bfloat16(y);
         }
     }
-    // nobody leaves while its partial sums are still read (they have been: what is added up is in registers); the stores of y need
-    // no ordering here, and waiting for them cost 1500 clocks
+    // nobody leaves while its partial sums are still read.  Every load of another CTA's memory above feeds a store, which is issued
+    // ahead of the arrival and only once the load has come back; so the arrival needs no release, which would wait for the stores
+    // of y as well (1500 clocks)
     if (o.split > 1) {
         __syncwarp();
         asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");

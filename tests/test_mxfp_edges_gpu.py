@@ -1,0 +1,32 @@
+"""MXFP4 products where tiles, lists and index ranges end."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_mxfp_gpu import TYPES, bound, host, matrix
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("M,cols,red", [(1, 44, 4096), (1, 300, 4096), (2, 172, 2100), (3, 129, 4096), (20, 4, 4096), (40, 260, 2048), (100, 133, 1030)])
+@pytest.mark.parametrize("what", ["linear", "grad", "product"])
+def test_split_reductions_whose_last_ranks_have_nothing_to_store(what, M, cols, red):
+    """A cluster shares out a tile's columns; past the last one its CTAs leave without having read each other's sums."""
+    import paper_2408_10746_b200 as pac
+    codes, scales, w = matrix(*((red, cols) if what == "grad" else (cols, red)), 5)
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(M, red, generator=g).bfloat16().cuda()
+    op, adds = (w if what == "grad" else w.T), red / 16 + 16
+    if what == "linear":
+        call = lambda: pac.mxfp_linear(x, codes, scales, torch.float32)  # noqa: E731
+    elif what == "grad":
+        call = lambda: pac.mxfp_linear_grad(x, codes, scales, cols, torch.float32)  # noqa: E731
+    else:
+        a = pac.quantize_mxfp(x)
+        x = pac.dequantize_mxfp(*a, red)
+        call = lambda: pac.mxfp_product(*a, codes, scales, red, torch.float32)  # noqa: E731
+    ref, size = host(x) @ op, np.abs(host(x)) @ np.abs(op)
+    first = call()
+    assert (np.abs(host(first) - ref) <= bound(ref, size, adds, TYPES["f32"])).all()
+    for _ in range(50):
+        assert torch.equal(call(), first)
