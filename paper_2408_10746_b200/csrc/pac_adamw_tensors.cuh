@@ -146,7 +146,8 @@ struct AtConst {
     uint32_t step_key;
 };
 
-// The 8-bit update of two elements: m and the root come decoded but for their block's constant, and leave as fp32.
+// The 8-bit update of two elements: m and the root come decoded but for their block's constant, and leave as fp32.  The root is
+// that of v for 0 and from 2^-126 to the largest number; at_update1 is for the rest.
 __device__ __forceinline__ void at_update2(float* p, float* m, float* v, const float* g, float ms, float vs, float wd, const AtStep& s, const AtConst& c) {
     const F2 gg = mul2(F2(g[0], g[1]), F2(s.grad_scale)), root = mul2(F2(v[0], v[1]), F2(vs));
     // every rounding as written above (the sums are scalar: the compiler fuses a packed sum with the product before it)
@@ -173,6 +174,23 @@ __device__ __forceinline__ void at_update2(float* p, float* m, float* v, const f
     const F2 pp(p[0], p[1]);
     fma2(mul2(F2(-c.lrbc1), F2(m[0], m[1])), F2(d[0], d[1]), fma2(F2(-wd), pp, pp)).get(p[0], p[1]);
 }
+// The same of element i from what is in memory, with a root that is right over all of fp32's range (subnormal v; v = infinity, whose
+// step is none).
+__device__ __forceinline__ float3 at_update1(const AtTensor& t, long long i, float ms, float vs, float wd, const AtStep& s, const AtConst& c) {
+    const float g = __fmul_rn(at_load1(t.g, i, t.flags & AT_G16), s.grad_scale), p = at_load1(t.p, i, t.flags & AT_P16);
+    const float m0 = __fmul_rn(at_decode1(static_cast<const unsigned char*>(t.m)[i]), ms), root = __fmul_rn(at_decode1(static_cast<const unsigned char*>(t.v)[i]), vs);
+    const float m = __fadd_rn(__fmul_rn(s.hp.beta1, m0), __fmul_rn(c.omb1, g));
+    const float v = __fsqrt_rn(__fadd_rn(__fmul_rn(s.hp.beta2, __fmul_rn(root, root)), __fmul_rn(__fmul_rn(c.omb2, g), g)));
+    return make_float3(__fmaf_rn(__fmul_rn(-c.lrbc1, m), __fdiv_rn(1.f, __fmaf_rn(v, c.rroot2, s.hp.eps)), __fmaf_rn(-wd, p, p)), m, v);
+}
+// Whether elements need it, from the largest of their roots.  A v below 2^-126 beside a root of 2^-40 or more does not: its
+// code is the smallest whatever its root (below 2^-18 of the block's largest it is rounded to 0 or that, and 0 becomes that), and in
+// the step eps hides a root below 2^-63 / sqrt(bc2), but for an eps below 2^25 times that (TINY: 1.2e-10 for beta2 = 0.999): then
+// every root is looked at.  (In every kernel that took the listed sizes 1 to 2 us more: 8.7 M elements 25 and 27 us.)  Blocks of
+// zeros do not come here, and in training hardly any do.
+__device__ __forceinline__ bool at_extreme(float top) { return !(top < __uint_as_float(0x7f800000u)) || (top < 9.094947e-13f && top > 0.f); }
+__device__ __forceinline__ bool at_small(float root) { return root < 1.08420217e-19f && root > 0.f; }    // 2^-63
+
 // Random bits of one element: the hash of its number ^ the block's key, from where the first xor-shift is done (x1).
 __device__ __forceinline__ uint32_t at_random(uint32_t x1) {
     uint32_t h = x1 * 0x85EBCA6Bu;
@@ -186,7 +204,7 @@ __device__ __forceinline__ void at_encode2(const float* m, const float* v, float
     at_codes2(F2(v[0], v[1]), F2(vf), __byte_perm(h0, 0u, 0x4324), __byte_perm(h1, 0u, 0x4324), vo[0], vo[1]);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        // a moment of -0 has no sign; a root above 0 is at least 2^-63, its bits are above 2^24, and its code is not 0
+        // a moment of -0 has no sign; a root above 0 is at least 2^-75, its bits are above 2^24, and its code is not 0
         mo[e] |= m[e] < 0.f ? 0x80000000u : 0u;
         vo[e] = max(vo[e], min(__float_as_uint(v[e]), 0x01000000u));
     }
@@ -194,85 +212,6 @@ __device__ __forceinline__ void at_encode2(const float* m, const float* v, float
 __device__ __forceinline__ bool at_finite(float top) { return top < __uint_as_float(0x7f800000u); }
 __device__ __forceinline__ float at_warp_top(float top) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))); }
 
-// 256 elements by a warp, eight consecutive ones per lane; all pointers aligned to eight elements.  What is read of a block,
-// as it lies in memory: the next block's are on their way while this one is computed (8 bits, 202 M bf16 elements: 697 us
-// without).
-template <int BITS, bool P16, bool G16>
-struct AtRaw {
-    uint32_t p[P16 ? 4 : 8], g[G16 ? 4 : 8], m[BITS == 32 ? 8 : 2], v[BITS == 32 ? 8 : 2];
-    float ms, vs;
-    __device__ __forceinline__ void load(const AtTensor& t, long long tb) {
-        const long long i = tb * AT_BLOCK + (threadIdx.x & 31) * 8;
-        at_load_words(g, static_cast<const char*>(t.g) + i * (G16 ? 2 : 4));
-        at_load_words(p, static_cast<const char*>(t.p) + i * (P16 ? 2 : 4));
-        at_load_words(m, static_cast<const char*>(t.m) + i * (BITS == 32 ? 4 : 1));
-        at_load_words(v, static_cast<const char*>(t.v) + i * (BITS == 32 ? 4 : 1));
-        if constexpr (BITS == 8) { ms = t.m_scale[tb]; vs = t.v_scale[tb]; }
-    }
-};
-template <int BITS, bool P16, bool G16>
-__device__ __forceinline__ void at_block(const AtTensor& t, long long tb, const AtRaw<BITS, P16, G16>& raw, uint32_t tensor_key, const AtStep& s, const AtConst& c) {
-    const int lane = threadIdx.x & 31;
-    const long long i = tb * AT_BLOCK + lane * 8;
-    float p[8], g[8], m[8], v[8];
-    at_values(raw.g, g);
-    at_values(raw.p, p);
-    if constexpr (BITS == 32) {
-        at_values(raw.m, m);
-        at_values(raw.v, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = adamw_math(p[j], m[j], v[j], __fmul_rn(g[j], s.grad_scale), t.flags & AT_DECAY, s.hp, c.bc1, c.bc2);
-        at_store8<false>(t.m, i, m);
-        at_store8<false>(t.v, i, v);
-        at_store8<P16>(t.p, i, p);
-    } else {
-        const float wd = (t.flags & AT_DECAY) ? c.lrwd : 0.f;
-        at_decode(make_uint2(raw.m[0], raw.m[1]), m);
-        at_decode(make_uint2(raw.v[0], raw.v[1]), v);
-        float mtop = 0.f, vtop = 0.f, mscale, vscale, mf, vf;
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            at_update2(p + j, m + j, v + j, g + j, raw.ms, raw.vs, wd, s, c);
-            mtop = at_top(at_top(mtop, m[j]), m[j + 1]);
-            vtop = at_top(at_top(vtop, v[j]), v[j + 1]);
-        }
-        at_store8<P16>(t.p, i, p);
-        mtop = at_warp_top(mtop);
-        vtop = at_warp_top(vtop);
-        at_constant(mtop, mscale, mf);
-        at_constant(vtop, vscale, vf);
-        // the hash of element ^ key; a lane's elements differ in the low byte only, so its first xor-shift is done once
-        const uint32_t x0 = (uint32_t)i ^ at_mix(tensor_key + (uint32_t)(i >> 32)), x1 = x0 ^ (x0 >> 16);
-        uint32_t mo[8], vo[8];
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) at_encode2(m + j, v + j, mf, vf, x1 ^ (uint32_t)j, x1 ^ (uint32_t)(j + 1), mo + j, vo + j);
-        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(t.m) + i) =
-            at_finite(mtop) ? make_uint2(at_pack(mo[0], mo[1], mo[2], mo[3]), at_pack(mo[4], mo[5], mo[6], mo[7])) : make_uint2(0u, 0u);
-        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(t.v) + i) =
-            at_finite(vtop) ? make_uint2(at_pack(vo[0], vo[1], vo[2], vo[3]), at_pack(vo[4], vo[5], vo[6], vo[7])) : make_uint2(0u, 0u);
-        if (lane == 0) { t.m_scale[tb] = mscale; t.v_scale[tb] = vscale; }
-    }
-}
-template <int BITS, bool P16, bool G16>
-__device__ __forceinline__ void at_blocks(const AtTensor& t, long long tb, long long end, uint32_t tensor_key, const AtStep& s, const AtConst& c) {
-    AtRaw<BITS, P16, G16> now;
-    if constexpr (BITS == 32) {                             // little to compute, and twice the words would not fit the registers
-#pragma unroll 1
-        for (; tb < end; ++tb) {
-            now.load(t, tb);
-            at_block<BITS, P16, G16>(t, tb, now, tensor_key, s, c);
-        }
-    } else {
-        now.load(t, tb);
-        AtRaw<BITS, P16, G16> next = now;
-#pragma unroll 1
-        for (; tb < end; ++tb) {
-            if (tb + 1 < end) next.load(t, tb + 1);
-            at_block<BITS, P16, G16>(t, tb, now, tensor_key, s, c);
-            now = next;
-        }
-    }
-}
 // The update of one element (and of a second one of zeros) from what is in memory.
 __device__ __forceinline__ void at_again(const AtTensor& t, long long i, bool g16, float ms, float vs, float wd, const AtStep& s, const AtConst& c,
                                          float (&p)[2], float (&m)[2], float (&v)[2]) {
@@ -281,6 +220,10 @@ __device__ __forceinline__ void at_again(const AtTensor& t, long long i, bool g1
     v[0] = at_decode1(static_cast<const unsigned char*>(t.v)[i]);
     m[1] = v[1] = 0.f;
     at_update2(p, m, v, g, ms, vs, wd, s, c);
+    if (at_extreme(v[0]) || at_small(v[0])) {
+        const float3 u = at_update1(t, i, ms, vs, wd, s, c);
+        p[0] = u.x; m[0] = u.y; v[0] = u.z;
+    }
 }
 // Up to 256 elements at any alignment, one of each 32 per lane.  8 bits: the moments are formed twice, for the maximum and for
 // the codes, from what is still in memory.
@@ -332,7 +275,98 @@ __device__ __forceinline__ void at_block_any(const AtTensor& t, long long tb, ui
     }
 }
 
-template <int BITS, int CAP>
+// 256 elements by a warp, eight consecutive ones per lane; all pointers aligned to eight elements.  What is read of a block,
+// as it lies in memory: the next block's are on their way while this one is computed (8 bits, 202 M bf16 elements: 697 us
+// without).
+template <int BITS, bool P16, bool G16>
+struct AtRaw {
+    uint32_t p[P16 ? 4 : 8], g[G16 ? 4 : 8], m[BITS == 32 ? 8 : 2], v[BITS == 32 ? 8 : 2];
+    float ms, vs;
+    __device__ __forceinline__ void load(const AtTensor& t, long long tb) {
+        const long long i = tb * AT_BLOCK + (threadIdx.x & 31) * 8;
+        at_load_words(g, static_cast<const char*>(t.g) + i * (G16 ? 2 : 4));
+        at_load_words(p, static_cast<const char*>(t.p) + i * (P16 ? 2 : 4));
+        at_load_words(m, static_cast<const char*>(t.m) + i * (BITS == 32 ? 4 : 1));
+        at_load_words(v, static_cast<const char*>(t.v) + i * (BITS == 32 ? 4 : 1));
+        if constexpr (BITS == 8) { ms = t.m_scale[tb]; vs = t.v_scale[tb]; }
+    }
+};
+template <int BITS, bool P16, bool G16, bool TINY>
+__device__ __forceinline__ bool at_block(const AtTensor& t, long long tb, const AtRaw<BITS, P16, G16>& raw, uint32_t tensor_key, const AtStep& s, const AtConst& c) {
+    const int lane = threadIdx.x & 31;
+    const long long i = tb * AT_BLOCK + lane * 8;
+    float p[8], g[8], m[8], v[8];
+    at_values(raw.g, g);
+    at_values(raw.p, p);
+    if constexpr (BITS == 32) {
+        at_values(raw.m, m);
+        at_values(raw.v, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = adamw_math(p[j], m[j], v[j], __fmul_rn(g[j], s.grad_scale), t.flags & AT_DECAY, s.hp, c.bc1, c.bc2);
+        at_store8<false>(t.m, i, m);
+        at_store8<false>(t.v, i, v);
+        at_store8<P16>(t.p, i, p);
+    } else {
+        const float wd = (t.flags & AT_DECAY) ? c.lrwd : 0.f;
+        at_decode(make_uint2(raw.m[0], raw.m[1]), m);
+        at_decode(make_uint2(raw.v[0], raw.v[1]), v);
+        float mtop = 0.f, vtop = 0.f, mscale, vscale, mf, vf;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            at_update2(p + j, m + j, v + j, g + j, raw.ms, raw.vs, wd, s, c);
+            mtop = at_top(at_top(mtop, m[j]), m[j + 1]);
+            vtop = at_top(at_top(vtop, v[j]), v[j + 1]);
+        }
+        bool again = false;
+        if constexpr (TINY) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) again |= at_small(v[j]);
+        }
+        mtop = at_warp_top(mtop);
+        vtop = at_warp_top(vtop);
+        if (at_extreme(vtop) || (TINY && __any_sync(0xffffffffu, again))) {
+            return false;
+        }
+        at_store8<P16>(t.p, i, p);
+        at_constant(mtop, mscale, mf);
+        at_constant(vtop, vscale, vf);
+        // the hash of element ^ key; a lane's elements differ in the low byte only, so its first xor-shift is done once
+        const uint32_t x0 = (uint32_t)i ^ at_mix(tensor_key + (uint32_t)(i >> 32)), x1 = x0 ^ (x0 >> 16);
+        uint32_t mo[8], vo[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) at_encode2(m + j, v + j, mf, vf, x1 ^ (uint32_t)j, x1 ^ (uint32_t)(j + 1), mo + j, vo + j);
+        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(t.m) + i) =
+            at_finite(mtop) ? make_uint2(at_pack(mo[0], mo[1], mo[2], mo[3]), at_pack(mo[4], mo[5], mo[6], mo[7])) : make_uint2(0u, 0u);
+        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(t.v) + i) =
+            at_finite(vtop) ? make_uint2(at_pack(vo[0], vo[1], vo[2], vo[3]), at_pack(vo[4], vo[5], vo[6], vo[7])) : make_uint2(0u, 0u);
+        if (lane == 0) { t.m_scale[tb] = mscale; t.v_scale[tb] = vscale; }
+    }
+    return true;
+}
+template <int BITS, bool P16, bool G16, bool TINY>
+__device__ __forceinline__ uint32_t at_blocks(const AtTensor& t, const long long first, long long end, uint32_t tensor_key, const AtStep& s, const AtConst& c) {
+    uint32_t left = 0;
+    long long tb = first;
+    AtRaw<BITS, P16, G16> now;
+    if constexpr (BITS == 32) {                             // little to compute, and twice the words would not fit the registers
+#pragma unroll 1
+        for (; tb < end; ++tb) {
+            now.load(t, tb);
+            at_block<BITS, P16, G16, TINY>(t, tb, now, tensor_key, s, c);
+        }
+    } else {
+        now.load(t, tb);
+        AtRaw<BITS, P16, G16> next = now;
+#pragma unroll 1
+        for (; tb < end; ++tb) {
+            if (tb + 1 < end) next.load(t, tb + 1);
+            if (!at_block<BITS, P16, G16, TINY>(t, tb, now, tensor_key, s, c)) left |= 1u << (tb - first);
+            now = next;
+        }
+    }
+    return left;
+}
+template <int BITS, int CAP, bool TINY>
 __global__ void __launch_bounds__(256, AT_CTAS) adamw_tensors_kernel(const __grid_constant__ AtList<CAP> list, const __grid_constant__ AtStep s) {
     __shared__ float bc_sh[2];
     AtConst k;
@@ -362,20 +396,20 @@ __global__ void __launch_bounds__(256, AT_CTAS) adamw_tensors_kernel(const __gri
         const uint32_t tensor_key = BITS == 8 ? at_mix(k.step_key + 0x9E3779B9u * (uint32_t)(s.first_tensor + lo + 1)) : 0u;
         const long long first = (long long)(c - t.first_chunk) * s.chunk, last = t.n / AT_BLOCK;
         const long long end = min(first + s.chunk, (t.n + AT_BLOCK - 1) / AT_BLOCK);
-        long long tb = first;
         const long long whole = (t.flags & AT_VEC) ? min(end, last) : first;
-        if (tb < whole) {
+        uint32_t left = 0;                                  // blocks ahead of `whole` that have yet to be done
+        if (first < whole) {
             if (t.flags & AT_P16) {
-                if (t.flags & AT_G16) at_blocks<BITS, true, true>(t, tb, whole, tensor_key, s, k);
-                else at_blocks<BITS, true, false>(t, tb, whole, tensor_key, s, k);
+                if (t.flags & AT_G16) left = at_blocks<BITS, true, true, TINY>(t, first, whole, tensor_key, s, k);
+                else left = at_blocks<BITS, true, false, TINY>(t, first, whole, tensor_key, s, k);
             } else {
-                if (t.flags & AT_G16) at_blocks<BITS, false, true>(t, tb, whole, tensor_key, s, k);
-                else at_blocks<BITS, false, false>(t, tb, whole, tensor_key, s, k);
+                if (t.flags & AT_G16) left = at_blocks<BITS, false, true, TINY>(t, first, whole, tensor_key, s, k);
+                else left = at_blocks<BITS, false, false, TINY>(t, first, whole, tensor_key, s, k);
             }
-            tb = whole;
         }
 #pragma unroll 1
-        for (; tb < end; ++tb) at_block_any<BITS>(t, tb, tensor_key, s, k);
+        for (long long tb = left ? first : whole; tb < end; ++tb)
+            if (tb >= whole || (left >> (tb - first) & 1u)) at_block_any<BITS>(t, tb, tensor_key, s, k);
     }
 }
 

@@ -383,7 +383,7 @@ namespace {
 
 unsigned long long blocks_of(const pac_adamw_tensor& t) { return (unsigned long long)((t.n + AT_BLOCK - 1) / AT_BLOCK); }
 
-template <int BITS, int CAP>
+template <int BITS, int CAP, bool TINY>
 cudaError_t launch_adamw(cudaStream_t st, const pac_adamw_tensor* t, int count, AtStep s, int sms) {
     AtList<CAP> list;
     unsigned long long blocks = 0, chunks = 0;
@@ -404,8 +404,12 @@ cudaError_t launch_adamw(cudaStream_t st, const pac_adamw_tensor* t, int count, 
     s.count = count;
     s.chunks = (uint32_t)chunks;
     const unsigned long long want = (chunks + 7) / 8, most = (unsigned long long)sms * 32;
-    adamw_tensors_kernel<BITS, CAP><<<(unsigned)(want < most ? want : most), 256, 0, st>>>(list, s);
+    adamw_tensors_kernel<BITS, CAP, TINY><<<(unsigned)(want < most ? want : most), 256, 0, st>>>(list, s);
     return cudaGetLastError();
+}
+template <int BITS, bool TINY>
+cudaError_t launch_list(cudaStream_t st, const pac_adamw_tensor* t, int count, const AtStep& s, int sms) {
+    return count <= AT_SMALL ? launch_adamw<BITS, AT_SMALL, TINY>(st, t, count, s, sms) : launch_adamw<BITS, AT_LARGE, TINY>(st, t, count, s, sms);
 }
 
 }  // namespace
@@ -439,6 +443,7 @@ extern "C" pac_status pac_adamw_tensors(int device, void* cuda_stream, const pac
         s.bc2 = (float)(1.0 - std::pow((double)hp->beta2, (double)step));
     }
     const int sms = sm_count(device);
+    const bool tiny = !((double)hp->eps * std::sqrt(1.0 - (double)hp->beta2) >= 3.637978807091713e-12);      // 2^(25 - 63); bc2 >= 1 - beta2
     for (int at = 0; at < count;) {
         // as many tensors as a list holds and whose blocks a 32-bit number counts; empty tensors only end a run
         int n = 0;
@@ -453,9 +458,9 @@ extern "C" pac_status pac_adamw_tensors(int device, void* cuda_stream, const pac
         }
         if (n == 0) break;
         s.first_tensor = at;
-        cudaError_t e;
-        if (n <= AT_SMALL) e = state_bits == 8 ? launch_adamw<8, AT_SMALL>(st, tensors + at, n, s, sms) : launch_adamw<32, AT_SMALL>(st, tensors + at, n, s, sms);
-        else e = state_bits == 8 ? launch_adamw<8, AT_LARGE>(st, tensors + at, n, s, sms) : launch_adamw<32, AT_LARGE>(st, tensors + at, n, s, sms);
+        const cudaError_t e = state_bits == 32 ? launch_list<32, false>(st, tensors + at, n, s, sms)
+                              : tiny           ? launch_list<8, true>(st, tensors + at, n, s, sms)
+                                               : launch_list<8, false>(st, tensors + at, n, s, sms);
         if (e != cudaSuccess) return PAC_ERR_CUDA;
         at += n;
     }
