@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(256) split_mxfp_kernel(const T* __restrict__ x
     pdl_trigger();
     const int lane = threadIdx.x & 31, pieces = mx_col_pieces(K), blocks = pieces * 4;
     const long long row_bytes = mx_row_bytes(K);
-    const int id = (int)((blockIdx.x * blockDim.x + threadIdx.x) >> 5), m = id / blocks, b = id - m * blocks;
+    const int id = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)), m = id / blocks, b = id - m * blocks;      // (threads may pass 32 bits, warps do not)
     if (m >= M) return;
     const int col = b * MX_BLOCK + lane;
     ms_terms(col < K ? to_f32(x[m * ldx + col]) : 0.f,

@@ -30,3 +30,23 @@ def test_split_reductions_whose_last_ranks_have_nothing_to_store(what, M, cols, 
     assert (np.abs(host(first) - ref) <= bound(ref, size, adds, TYPES["f32"])).all()
     for _ in range(50):
         assert torch.equal(call(), first)
+
+
+def test_few_tokens_of_more_than_32_bits_of_values():
+    """16 tokens of 2^28 + 512 columns: the last 8192 of the last token are beyond 2^32 values of x."""
+    import paper_2408_10746_b200 as pac
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    M, N, K = 16, 4, 2 ** 28 + 512
+    codes = torch.full((N, K // 2), 0x22, dtype=torch.uint8, device="cuda")          # 1 everywhere
+    codes[1] = 0x44                                              # 2
+    scales = torch.full(pac.mxfp_shapes(N, K)[1], 127, dtype=torch.uint8, device="cuda")
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    x[15, -8192:] = (torch.arange(8192, device="cuda") % 64).bfloat16()              # whole numbers: every sum is exact
+    x[3, :64] = 1
+    x[15, 0] = 5
+    y = pac.mxfp_linear(x, codes, scales, torch.float32)
+    want = torch.zeros(M, N, device="cuda")
+    want[3], want[15] = 64, 5 + 128 * 2016
+    want[:, 1] *= 2
+    assert torch.equal(y, want)
