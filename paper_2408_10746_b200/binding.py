@@ -520,6 +520,9 @@ def _stream(index: int) -> int:
     return _RAW_STREAM(index)
 
 
+_MXFP_MOST = 0x7fffff00                                       # rows or columns; a C int would cut larger numbers off in silence
+
+
 def _rows(t, name: str):
     """A CUDA matrix with consecutive elements along its rows: (rows, columns, elements from row to row)."""
     if not t.is_cuda or t.dim() != 2:
@@ -527,6 +530,8 @@ def _rows(t, name: str):
     rows, cols = t.shape
     if cols < 1:
         _refuse(f"{name} has at least one column")
+    if rows > _MXFP_MOST or cols > _MXFP_MOST:
+        _refuse(f"{name} has at most {_MXFP_MOST} rows and columns")
     ld, step = t.stride()
     if cols > 1 and step != 1 and rows:
         _refuse(f"{name}: elements of a row are consecutive")
@@ -549,6 +554,8 @@ def _mxfp(codes, scales, cols: int, device=None):
             and codes.is_contiguous() and scales.is_contiguous() and cols > 0):
         _refuse("codes and scales are contiguous CUDA uint8 tensors")
     rows, width = codes.shape
+    if rows > _MXFP_MOST or cols > _MXFP_MOST:
+        _refuse(f"a matrix has at most {_MXFP_MOST} rows and columns")
     if width != 16 * ((cols + 31) // 32) or scales.shape != ((rows + 127) // 128, 2 * ((cols + 255) // 256), 32, 4, 4):
         _refuse(f"{rows} x {cols} values have codes and scales of shapes {mxfp_shapes(rows, cols)}, not {tuple(codes.shape)} and {tuple(scales.shape)}")
     at = codes.device
