@@ -580,13 +580,26 @@ def _span(t):
     return a, a + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size() if t.numel() else a
 
 
+def _row_bytes(t):
+    """(bytes of a row, bytes from row to row or 0 where there is one row) of a matrix or a contiguous tensor."""
+    e = t.element_size()
+    if t.dim() != 2 or t.shape[0] <= 1:
+        return (t.numel() if t.dim() != 2 else t.shape[1]) * e, 0
+    return t.shape[1] * e, t.stride()[0] * e
+
+
 def _apart(out, *inputs):
-    """A result that the caller provides lies apart from what the call reads."""
+    """A result that the caller provides lies apart from what the call reads: in another place, or in other columns of the same rows."""
     a, b = _span(out)
     for t in inputs:
         c, d = _span(t)
-        if a < d and c < b:
-            _refuse("the result does not overlap the inputs")
+        if a < b and c < d and a < d and c < b:
+            (w, p), (v, q) = _row_bytes(out), _row_bytes(t)
+            pitch = p or q
+            # both lie in rows `pitch` apart (one that is a single row may begin anywhere): columns [0, w) and [at, at + v), in turn
+            at = (c - a) % pitch if pitch else 0
+            if not pitch or (p and q and p != q) or at < w or at + v > pitch:
+                _refuse("the result does not overlap the inputs")
 
 
 def quantize_mxfp(x, codes=None, scales=None):

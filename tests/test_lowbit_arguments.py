@@ -50,3 +50,47 @@ def test_sizes_beyond_32_bits_are_refused_and_not_cut(n):
         with pytest.raises(pac.PacError) as e:
             call()
         assert e.value.status_name == "PAC_ERR_INVALID_ARG"
+
+
+def view(at, rows, cols, pitch, dtype=torch.bfloat16):
+    return Shape((rows, cols), dtype, (pitch, 1), at)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_columns_of_one_buffer_beside_each_other_lie_apart(dtype):
+    """A result and an input as column slices of the same rows: their spans cross, their elements do not."""
+    e, P = dtype.itemsize, 200
+    x = view(4096, 6, 64, P, dtype)
+    fine = [(64, 6, 136), (64, 6, 40), (100, 6, 40), (100, 3, 40), (264, 5, 100), (P * 3 + 64, 2, 136), (64, 1, 136), (P * 5 + 64, 9, 136), (6 * P - 136, 4, 136)]
+    for first, rows, cols in fine:
+        binding._apart(view(4096 + e * first, rows, cols, P, dtype), x)
+        binding._apart(x, view(4096 + e * first, rows, cols, P, dtype))
+    for first, rows, cols in [(0, 6, 64), (63, 6, 40), (40, 1, 10), (100, 6, 101), (P - 10, 3, 11), (P * 2, 1, 1), (P * 5 + 63, 1, 1)]:
+        for a, b in ((view(4096 + e * first, rows, cols, P, dtype), x), (x, view(4096 + e * first, rows, cols, P, dtype))):
+            with pytest.raises(pac.PacError):
+                binding._apart(a, b)
+
+
+def test_overlaps_are_those_of_the_elements():
+    """Against the sets of elements, over places, widths and pitches."""
+    import random
+    rng = random.Random(1)
+    seen = [0, 0]
+    for _ in range(4000):
+        P = rng.randint(4, 12)
+        a = (rng.randint(0, 40), rng.randint(0, 4), rng.randint(1, P), P)
+        Q = P if rng.random() < 0.7 else rng.randint(4, 12)
+        b = (rng.randint(0, 40), rng.randint(0, 4), rng.randint(1, Q), Q)
+        cells = [{at + r * p + c for r in range(rows) for c in range(cols)} for at, rows, cols, p in (a, b)]
+        meet = bool(cells[0] & cells[1])
+        args = [view(4096 + 2 * at, rows, cols, p) for at, rows, cols, p in (a, b)]
+        try:
+            binding._apart(*args)
+            refused = False
+        except pac.PacError:
+            refused = True
+        assert refused or not meet                               # never an overlap let through
+        if P == Q or min(a[1], b[1]) <= 1:
+            assert refused == meet, (a, b)                       # rows of one buffer: exactly the overlaps (others: when their spans cross)
+        seen[refused] += 1
+    assert min(seen) > 400

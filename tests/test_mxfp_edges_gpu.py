@@ -50,3 +50,27 @@ def test_few_tokens_of_more_than_32_bits_of_values():
     want[3], want[15] = 64, 5 + 128 * 2016
     want[:, 1] *= 2
     assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M", [1, 5, 40, 700])
+def test_results_beside_their_inputs_in_one_buffer(M, dtype):
+    """x in the first columns of a buffer, y, dx and values read back in others; what lies between stays as it was."""
+    import paper_2408_10746_b200 as pac
+    N, K = 300, 520
+    codes, scales, w = matrix(N, K, 8)
+    g = torch.Generator().manual_seed(2)
+    buf = torch.randn(M, 2600, generator=g).to(dtype).cuda()
+    before, apart = buf.clone(), buf[:, :K].clone()
+    x, y, dx, back = buf[:, :K], buf[:, 600:600 + N], buf[:, 1000:1000 + K], buf[:, 2000:2000 + K]
+    want_y = pac.mxfp_linear(apart, codes, scales)
+    want_dx = pac.mxfp_linear_grad(want_y, codes, scales, K)
+    pac.mxfp_linear(x, codes, scales, out=y)
+    pac.mxfp_linear_grad(y, codes, scales, K, out=dx)
+    held = pac.quantize_mxfp(x)
+    pac.dequantize_mxfp(*held, K, out=back)
+    assert torch.equal(y, want_y) and torch.equal(dx, want_dx) and torch.equal(back, pac.dequantize_mxfp(*pac.quantize_mxfp(apart), K, dtype))
+    for t in (y, dx, back):
+        first = t.storage_offset()
+        t.copy_(before[:, first:first + t.shape[1]])
+    assert torch.equal(buf, before)
