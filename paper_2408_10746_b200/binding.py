@@ -643,7 +643,15 @@ def dequantize_mxfp(codes, scales, cols: int, dtype=None, out=None):
     return out
 
 
+def _no_graph(*tensors):
+    """The products record no graph, so a gradient that is asked for is refused instead of lost."""
+    import torch
+    if any(t.requires_grad for t in tensors) and torch.is_grad_enabled():
+        _refuse("the call records no gradient: run it under torch.no_grad(), or in an autograd.Function whose backward pass is mxfp_linear_grad")
+
+
 def _mxfp_linear(call, lib, x, M: int, ld: int, codes, scales, N: int, K: int, grad: bool, dtype, out):
+    _no_graph(x) if out is None else _no_graph(x, out)
     dtype = dtype or (out.dtype if out is not None else x.dtype)
     device, xt, yt, at = x.device, _dtype(x.dtype), _dtype(dtype), x.data_ptr()
     if out is not None:
@@ -659,7 +667,8 @@ def _mxfp_linear(call, lib, x, M: int, ld: int, codes, scales, N: int, K: int, g
 
 
 def mxfp_linear(x, codes, scales, dtype=None, out=None):
-    """y = x W^T [M][N] for x [M][K] and a frozen W [N][K] in MXFP4 (quantize_mxfp); x and y float32 or bfloat16."""
+    """y = x W^T [M][N] for x [M][K] and a frozen W [N][K] in MXFP4 (quantize_mxfp); x and y float32 or bfloat16.  No graph is
+    recorded (an x that requires a gradient is refused under grad mode; mxfp_linear_grad is the backward pass)."""
     M, K, ld = _rows(x, "x")
     N = _mxfp(codes, scales, K, x.device)
     if N < 1:

@@ -8,7 +8,7 @@ from paper_2408_10746_b200 import binding
 
 class Shape:
     """A CUDA tensor's shape and place; reading its address says that the call went on to the kernel."""
-    is_cuda, device = True, torch.device("cuda", 0)
+    is_cuda, device, requires_grad = True, torch.device("cuda", 0), False
 
     def __init__(self, shape, dtype=torch.bfloat16, stride=None, at=None):
         self.shape, self.dtype, self.at = tuple(shape), dtype, at
@@ -94,3 +94,19 @@ def test_overlaps_are_those_of_the_elements():
             assert refused == meet, (a, b)                       # rows of one buffer: exactly the overlaps (others: when their spans cross)
         seen[refused] += 1
     assert min(seen) > 400
+
+
+@pytest.mark.parametrize("call", [lambda x, m, out: pac.mxfp_linear(x, *m, out=out), lambda x, m, out: pac.mxfp_linear_grad(x, *m, 64, out=out)])
+def test_a_gradient_is_not_lost_in_silence(call):
+    """The calls record no graph: under grad mode they refuse what requires a gradient, and go on with it without."""
+    m = matrix(64, 64)
+    needs, plain = Shape((4, 64)), Shape((4, 64))
+    needs.requires_grad = True
+    for x, out in ((needs, None), (plain, needs)):
+        with pytest.raises(pac.PacError) as e:
+            call(x, m, out)
+        assert e.value.status_name == "PAC_ERR_INVALID_ARG" and "gradient" in str(e.value)
+    with torch.no_grad(), pytest.raises(AssertionError, match="went on"):
+        call(needs, m, None)
+    with pytest.raises(AssertionError, match="went on"):
+        call(plain, m, None)

@@ -74,3 +74,29 @@ def test_results_beside_their_inputs_in_one_buffer(M, dtype):
         first = t.storage_offset()
         t.copy_(before[:, first:first + t.shape[1]])
     assert torch.equal(buf, before)
+
+
+def test_as_an_autograd_function():
+    """How a graph is recorded: the forward call runs without grad mode inside a Function, whose backward pass is the gradient's call."""
+    import paper_2408_10746_b200 as pac
+    codes, scales, w = matrix(300, 200, 3)
+
+    class Frozen(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return pac.mxfp_linear(x, codes, scales)
+
+        @staticmethod
+        def backward(ctx, dy):
+            return pac.mxfp_linear_grad(dy.contiguous(), codes, scales, 200)
+
+    x = torch.randn(20, 200, device="cuda", requires_grad=True)
+    with pytest.raises(pac.PacError):
+        pac.mxfp_linear(x, codes, scales)
+    y = Frozen.apply(x)
+    dy = torch.randn(20, 300, device="cuda")
+    y.backward(dy)
+    ref, size = host(dy) @ w, np.abs(host(dy)) @ np.abs(w)
+    assert (np.abs(host(x.grad) - ref) <= bound(ref, size, 300 / 16 + 16, torch.float32)).all()
+    held = pac.quantize_mxfp(torch.nn.Parameter(torch.randn(40, 64, device="cuda")))          # codes have no gradient: nothing is lost
+    assert held[0].shape == (40, 32)
