@@ -5,16 +5,18 @@
 // 8 bits: m and sqrt(v) are kept as float8 (E4M3) times an fp32 constant per 256 elements, absmax / 448.  The root halves
 // the range of exponents that has to fit.  With beta2 = 0.999 a step moves v by a thousandth and neighbouring codes are
 // an eighth apart, so rounding to the nearest would hold v where it is for ever; codes are rounded up or down by 16
-// random bits instead (up with the probability of the remainder), which keeps what is stored unbiased.  The bits are a hash
+// random bits instead (up with the probability of the remainder), which keeps m and the root unbiased.  v, the root's square, has
+// the rounding's variance on top of it: after 4000 steps 5 % too much on average, and 17 % of noise in the root.  The bits are a hash
 // of (seed, step, tensor, element): the same call gives the same codes.  A root that is not 0 never becomes 0, so a
-// moment never meets a denominator of eps alone.  A block with a gradient that is not finite gets the constant NaN.
+// moment never meets a denominator of eps alone; what lies below 1 / 229376 of its block's largest is held too large for that.  A
+// block with a gradient that is not finite gets the constant NaN.
 //
 // The step reads and writes every element once: 28 bytes (fp32 everywhere), 16 (moments in 8 bits), 10 (bf16 parameters
 // and gradients on top).  A warp takes 256 elements, eight per lane, so the block's maximum is five shuffles and the
 // moments never leave its registers between decoding and encoding.  The list is an argument of the kernel (constant
 // memory): nothing to copy, nothing to keep alive after the call, capturable.
 //
-// Measured, 202 M elements: 510 us with fp32 parameters and 8-bit moments (6.3 TB/s), 426 us with bf16 ones (4.7 TB/s: half
+// Measured, 202 M elements: 512 us with fp32 parameters and 8-bit moments (6.3 TB/s), 459 us with bf16 ones (4.4 TB/s: half
 // the bytes in flight for the same 60 instructions an element; two blocks ahead do not fit the registers, 487 us and more); fp32 everywhere 50 M in 238 us (5.9 TB/s).
 #pragma once
 #include "pac_ptx.cuh"
@@ -42,7 +44,8 @@ struct AtStep {
     const long long* dev_step;  // when given: the number of the step, in place of step, bc1, bc2
 };
 
-// A bijection of 32 bits whose every output bit depends on every input bit: two multiplications between xor-shifts.
+// A bijection of 32 bits whose every output bit depends on every input bit: the finaliser of MurmurHash3 (Austin Appleby, public
+// domain), two multiplications between xor-shifts, with its published constants.
 __host__ __device__ __forceinline__ uint32_t at_mix(uint32_t x) {
     x ^= x >> 16; x *= 0x85EBCA6Bu;
     x ^= x >> 13; x *= 0xC2B2AE35u;
@@ -163,8 +166,8 @@ __device__ __forceinline__ void at_update2(float* p, float* m, float* v, const f
         asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(d[k]) : "f"(fmaxf(v[k], 1.17549435e-38f)));
     }
     // sqrt(v): the hardware's y = 1 / sqrt(v) and one step of Newton's method on r^2 = v in fused arithmetic, r = vy,
-    // r + (v - r^2) y / 2, which leaves 2^-45 before its rounding.  (202 M bf16 elements: 426 us; 396 with the hardware's
-    // approximate root and fused sums, whose codes and constants then differ from the definition's here and there.)
+    // r + (v - r^2) y / 2, which leaves 2^-45 before its rounding.  (With the hardware's approximate root and fused sums 7 %
+    // less time, but codes and constants that differ from the definition's here and there.)
     const F2 y(d[0], d[1]), vv(v[0], v[1]), r = mul2(vv, y), nr = mul2(vv, mul2(y, F2(-1.f)));
     fma2(fma2(nr, r, vv), mul2(y, F2(0.5f)), r).get(v[0], v[1]);
     // the root is at hand for the step too, whose corrections are factors: a reciprocal (1 ulp) is left

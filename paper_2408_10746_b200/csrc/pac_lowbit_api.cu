@@ -256,9 +256,9 @@ pac_status mxfp_linear(bool grad, int device, void* stream, const void* x, int x
     };
     const long long w_tiles = (out_cols + 127LL) / 128, units = (w_tiles + 1) / 2 * ((M + 255LL) / 256);
     // pairs where their tiles fill more than half of the SMs (4096 x 4096: 512 tokens, 32 tiles, 33 us in pairs and 25 in tiles of one CTA
-    // with a split reduction; 1024 tokens, 64 tiles, 34 either way, 34 and 58 with fp32 results); fp32 results up to where two accumulators take 128
-    // additions each
-    if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (!y_f32 || red <= 4096)) {
+    // with a split reduction; 1024 tokens, 64 tiles, 34 either way, 34 and 58 with fp32 results); fp32 results up to where two accumulators take
+    // MX_ADDS_F32 additions each (of an fp32 x's first term: see pac_mxfp_pair.cuh)
+    if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (!y_f32 || red <= 2 * 16 * MX_ADDS_F32)) {
         MrParams r = {};
         r.y = y; r.ldy = ldy; r.y_f32 = y_f32; r.scales = scales;
         r.M = M; r.cols = out_cols; r.red = red; r.pieces = mx_col_pieces(K); r.red_tiles = (int)((red + 127LL) / 128);
@@ -291,7 +291,7 @@ extern "C" pac_status pac_quantize_mxfp(int device, void* cuda_stream, const voi
     if (!on.ok) return PAC_ERR_CUDA;
     const bool vec = aligned(dev_x, 32) && (ldx * (long long)dtype_size(dtype)) % 32 == 0;
     const long long items = (rows + MX_TILE - 1) / MX_TILE * (MX_TILE / 4) * (mx_col_pieces(cols) / 2);
-    const long long want = (items + 7) / 8, most = 148LL * 32;
+    const long long want = (items + 7) / 8, most = sm_count(device) * 32LL;
     const unsigned grid = (unsigned)(want < most ? want : most);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const MxDiv by_pairs(mx_col_pieces(cols) / 2, items);
@@ -309,7 +309,7 @@ extern "C" pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const u
     if (!on.ok) return PAC_ERR_CUDA;
     const bool vec = aligned(dev_out, 32) && (ldo * (long long)dtype_size(dtype)) % 32 == 0;
     const long long per_row = mx_row_bytes(cols) / (vec ? 8 : 1), items = rows * per_row;
-    const long long want = (items + 255) / 256, most = 148LL * 32;
+    const long long want = (items + 255) / 256, most = sm_count(device) * 32LL;
     const unsigned grid = (unsigned)(want < most ? want : most);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const MxDiv by_row(per_row, items);
@@ -353,8 +353,8 @@ extern "C" pac_status pac_mxfp_product(int device, void* cuda_stream, const unsi
     cudaError_t e;
     const long long units = (N + 255LL) / 256 * ((M + 255LL) / 256);
     // pairs where their tiles fill more than half of the SMs (4096 x 4096: 512 tokens 12 us either way, 2048 tokens 19 in pairs and 26 in
-    // tiles of one CTA); fp32 results up to 128 additions into an accumulator
-    if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (y_dtype != PAC_F32 || K <= 8192)) {
+    // tiles of one CTA); fp32 results up to MX_ADDS_F32 additions into its accumulator
+    if (M > 128 && units * 4 > sms && units <= 0x7fffffffLL && (y_dtype != PAC_F32 || K <= 64 * MX_ADDS_F32)) {
         MqParams q = {};
         q.y = dev_y; q.ldy = ldy; q.y_f32 = y_dtype == PAC_F32; q.M = M; q.cols = N; q.steps = (int)((K + 255LL) / 256);
         q.w_units = (int)((N + 255LL) / 256); q.t_units = (int)((M + 255LL) / 256);

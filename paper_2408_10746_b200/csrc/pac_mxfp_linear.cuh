@@ -21,8 +21,9 @@
 // tensor cores: see pac_mxfp_pair.cuh.
 //
 // Precision: operands exact, sums in fp32.  The tensor core cuts partial sums instead of rounding them, so K steps take
-// turns over the accumulators that tensor memory has room for.  x in fp32 enters as three bf16 terms that add up to it
-// exactly; the second and third share an accumulator.
+// turns over the accumulators that tensor memory has room for (MX_ADDS_F32 below).  x in fp32 enters as three bf16 terms that
+// add up to it exactly (below 2^-110 the third one ends at bf16's smallest number: to 2^-134); the second and third share an
+// accumulator, whose additions are twice as many and cut 2^-8 as much.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -218,7 +219,7 @@ __device__ __forceinline__ void mx_finish(const MxOut& o, uint32_t tmem_base, un
 }
 
 // x as TMA boxes can read it: TERMS matrices [rows][16-byte rows of whole 128-column pieces] in bf16, below one another.  A bf16 x
-// whose rows do not begin on 16-byte boundaries is copied; an fp32 x becomes three bf16 terms that add up to it exactly.
+// whose rows do not begin on 16-byte boundaries is copied; an fp32 x becomes three bf16 terms that add up to it (see above).
 __host__ __device__ inline int pack_columns(int red) { return (red + 127) / 128 * 128; }
 template <typename T>
 __global__ void __launch_bounds__(256) pack_tokens_kernel(const T* __restrict__ x, int M, int red, long long ldx, bool vec, bf16* __restrict__ out) {

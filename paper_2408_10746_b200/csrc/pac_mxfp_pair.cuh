@@ -3,7 +3,7 @@
 // converted once per 256 tokens and a K step of 64 costs an SM 8192 conversions and 20 KB from L2 for 512 clocks of tensor work;
 // alone it would be the same conversions and 36 KB.  Persistent pairs; the accumulators of one tile are stored while the
 // next tile is computed (bf16 results), or both halves of tensor memory take turns within a tile (fp32 results: half the
-// additions into either).  A reduction of more additions than a bf16 result's accumulator takes is computed in equal parts: one
+// additions into either, counting those of an fp32 x's first term; the other two come first and cut 2^-8 as much).  A reduction of more additions than a bf16 result's accumulator takes is computed in equal parts: one
 // half of tensor memory receives a part, the storing warps add it to the sum of the parts before it, which the other half holds.  An fp32 x comes as three bf16 terms and the reduction goes over W three times, the smallest term first: what
 // is cut off while the sums are small is smaller still.
 //

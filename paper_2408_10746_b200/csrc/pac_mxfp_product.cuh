@@ -57,9 +57,9 @@ __device__ __forceinline__ uint32_t instr_desc_mxf4(int M, int N, uint32_t half)
 }
 
 // A block of x, a value per lane, as a sum of MS_TERMS blocks in MXFP4: the first is x rounded, each next one is what the ones
-// before it leave, rounded with a scale two powers of two finer.  What a term leaves is at most 2 of its units (of [6, 8), which
+// before it leave, rounded with a scale two powers of two finer, 2^-127 at the least.  What a term leaves is at most 2 of its units (of [6, 8), which
 // become 6; else at most 1), so it is below 8 of the next one's, and the twelfth leaves at most 2^-23 of the largest of the 32
-// (mostly 2^-26): bf16 values within 2^14 of each other enter exactly.  With it the products of a few tokens are block-scaled
+// (mostly 2^-26; 2^-129 where scales end): bf16 values within 2^14 of each other enter exactly.  With it the products of a few tokens are block-scaled
 // products of the codes of W as they are: nothing converts W, whose bytes are the floor.  (Scales from the remainders' own
 // largest gain 0.6 bits a term and cost a reduction over the warp in each of the twelve dependent rounds: twice the time.)
 // put_codes(term, word): the codes of this lane's eight neighbours (lane / 8); put_scale(term, byte).  Terms 8 .. 11 come with
@@ -247,7 +247,8 @@ __global__ void __launch_bounds__(320, 2) mxfp_product_kernel(const __grid_const
 }
 
 // One or two tokens whose terms are made in the product's own kernel, which saves a launch and the workspace: how many CTAs
-// share a reduction (two CTAs on each of 148 SMs), and whether what each has to make is little enough (a step of 256 columns and
+// share a reduction (two CTAs on each of B200's 148 SMs; a constant, since the size of the workspace is asked for without naming
+// a device), and whether what each has to make is little enough (a step of 256 columns and
 // one token is about 1000 clocks of 12 dependent rounds).
 constexpr int MS_HERE_CTAS = 296;
 inline int ms_here_split(int N, int K) {

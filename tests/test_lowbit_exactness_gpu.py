@@ -165,3 +165,25 @@ def test_what_lies_far_below_a_blocks_largest_moment_is_held_too_large():
     held = s["v"][0].float() * s["v_scale"][0]
     assert (s["v"][0].view(torch.uint8)[1:] == 1).all()
     assert abs(float(held[0] / held[1]) - 229376) < 1 and float(held[1]) > 1e2 * 1e-9 * 0.001 ** 0.5
+
+
+@pytest.mark.parametrize("M", [1, 2, 16, 20, 130])
+def test_tokens_near_the_end_of_fp32s_range(M):
+    """The smallest scale is 2^-127 and the smallest bf16 2^-133: few tokens enter to 2^-23 of the largest of 32 or to 2^-129, fp32 ones of
+    more tokens to 2^-134, and exactly from 2^-110 on.  W is 2^60 times an identity, so that the results are normal numbers."""
+    import paper_2408_10746_b200 as pac
+    n = 2048
+    codes, scales = identity(n)
+    scales += 60
+    g = torch.Generator().manual_seed(M)
+    size = torch.exp2(torch.randint(-140, -90, (M, n // 32), generator=g).float()).repeat_interleave(32, 1)
+    x = (torch.randn(M, n, generator=g) * size).cuda()
+    y = pac.mxfp_linear(x, codes, scales).double()
+    want = x.double() * 2.0 ** 60
+    if M <= 16:
+        top = x.double().abs().view(M, -1, 32).amax(2).repeat_interleave(32, 1)
+        off = (2.0 ** -23 * top).clamp(min=2.0 ** -129)
+    else:
+        off = torch.where(x.abs() < 2.0 ** -110, 2.0 ** -134, 0.0).double()
+    # a cut of 2^-22 of the sum for each of the three or twelve terms
+    assert ((y - want).abs() <= 2.0 ** 60 * off + 12 * 2.0 ** -22 * want.abs()).all(), ((y - want).abs() / 2.0 ** 60).max()
