@@ -344,8 +344,8 @@ pac_status pac_dequantize_absmax(int device, void* cuda_stream, const signed cha
  * These calls and those below enqueue on cuda_stream (NULL: the default stream) of `device`, leave the caller's current device
  * as it was, allocate nothing, keep nothing and may be captured into a graph.  No rows: nothing is done.  Errors:
  * PAC_ERR_INVALID_ARG for NULL or misaligned pointers, unknown types, cols < 1 or a pitch below it; PAC_ERR_UNSUPPORTED for more
- * rows than a launch has tiles (some 4 million of an fp32 x, 8 million of another, where an fp32 result sums over more columns than
- * stated below); PAC_ERR_CUDA.  Results do not overlap inputs; other columns of the same rows are another place. */
+ * rows than a launch has tiles (some 4 million of an fp32 x and 8 million of another one, where an fp32 result sums over more than
+ * 4096 columns, or 8192 in pac_mxfp_product); PAC_ERR_CUDA.  Results do not overlap inputs; other columns of the same rows are another place. */
 pac_status pac_quantize_mxfp(int device, void* cuda_stream, const void* dev_x, int dtype, long long rows, int cols, long long ldx,
                              unsigned char* dev_codes, unsigned char* dev_scales);
 pac_status pac_dequantize_mxfp(int device, void* cuda_stream, const unsigned char* dev_codes, const unsigned char* dev_scales,

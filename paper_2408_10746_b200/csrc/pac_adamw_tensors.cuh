@@ -16,8 +16,9 @@
 // moments never leave its registers between decoding and encoding.  The list is an argument of the kernel (constant
 // memory): nothing to copy, nothing to keep alive after the call, capturable.
 //
-// Measured, 202 M elements: 512 us with fp32 parameters and 8-bit moments (6.3 TB/s), 459 us with bf16 ones (4.4 TB/s: half
-// the bytes in flight for the same 60 instructions an element; two blocks ahead do not fit the registers, 487 us and more); fp32 everywhere 50 M in 238 us (5.9 TB/s).
+// Measured, 202 M elements: 512 us with fp32 parameters and 8-bit moments (6.3 TB/s), 459 us with bf16 ones (4.4 TB/s: the
+// same 60 instructions an element for half the bytes, 80 % of the issue slots; two blocks ahead do not fit the registers, 487 us and
+// more); fp32 everywhere 50 M in 228 us (6.2 TB/s), with bf16 parameters and gradients 197.
 #pragma once
 #include "pac_ptx.cuh"
 #include "pac_adamw.cuh"
